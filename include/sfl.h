@@ -451,6 +451,175 @@ sfl_status_t sfl_transpose(const void* in, void* out, int64_t rows, int64_t cols
  * d / split is 512, 1024, 2048 or 4096. */
 sfl_status_t sfl_down_projection_rowwise(const sfl_ffn_args_t* args, int32_t split, sfl_stream_t stream);
 
+/* ---- Around the layer: a routed residual block ------------------------------------------
+ * The operators that a model has beside the layer when it uses it as a residual block, with a
+ * router over several experts (each expert one call of the layer on its share of the rows), and
+ * when it trains it. The conventions above hold: caller-owned contiguous row-major buffers, no
+ * allocation, no synchronisation, errors before any launch. Rows are bf16 or fp32 (dtype);
+ * parameters, gates, weights and their gradients are fp32; sums are held in fp32 (the gradient
+ * norm in fp64) in a fixed order, so results are the same from call to call. Pointers need the
+ * alignment of their element type only; a row of any width is served. */
+
+/* Which norms a block's boundary has. */
+enum {
+  SFL_NORM_PRE = 1, /* of the new residual stream, for the next block */
+  SFL_NORM_POST = 2 /* of the block's output */
+};
+
+/* Arguments of sfl_norm_forward: RMS norms, gates and residual sum between two blocks. Per row t,
+ *   P = Y r_y w_post, r_y = 1 / sqrt(mean(Y[t]^2) + eps)   (SFL_NORM_POST; else P = Y)
+ *   X_out = res_scale X + gate_t[t] gate_c P
+ *   N = X_out r_x w_pre, r_x = 1 / sqrt(mean(X_out[t]^2) + eps)   (SFL_NORM_PRE)
+ * N is formed from X_out before its rounding to dtype.
+ *  norms   SFL_NORM_* bits
+ *  T, d    rows and width, d <= 16384
+ *  eps     added to the mean square, >= 0
+ *  X       [T][d] residual stream
+ *  Y       [T][d] the block's output; NULL where there is none (before the first block):
+ *          X_out = res_scale X; w_post and the gates have to be NULL and SFL_NORM_POST unset then
+ *  w_pre, w_post   [d] fp32 norm weights, NULL for ones
+ *  gate_c, gate_t  [d] and [T] fp32 gates per channel and per token, NULL for ones
+ *  X_out   [T][d], may be X (in place); NULL where it is not wanted (SFL_NORM_PRE only)
+ *  N       [T][d], with SFL_NORM_PRE; overlaps no input */
+typedef struct {
+  sfl_dtype_t dtype;
+  int32_t norms;
+  int64_t T, d;
+  float eps;
+  float res_scale;
+  const void* X;
+  const void* Y;
+  const float* w_pre;
+  const float* w_post;
+  const float* gate_c;
+  const float* gate_t;
+  void* X_out;
+  void* N;
+} sfl_norm_args_t;
+
+/* Arguments of sfl_norm_backward: gradients of sum(dX_out * X_out) + sum(dN * N).
+ *  norms to gate_t   as in the forward; X_out as the forward stored it (read with SFL_NORM_PRE)
+ *  dX_out, dN  [T][d] gradients of X_out and N; NULL for zeros (dN: only with SFL_NORM_PRE)
+ *  dX      [T][d] gradient of X, may be dX_out (in place), or NULL
+ *  dY      [T][d] gradient of Y, overlaps no input, or NULL
+ *  dw_pre, dw_post, dgate_c [d], dgate_t [T]   fp32, overwritten, each NULL where it is not
+ *          wanted (a gradient of a weight that was NULL is that of a weight of ones)
+ *  workspace   sfl_norm_workspace_size() bytes, 4-byte aligned */
+typedef struct {
+  sfl_dtype_t dtype;
+  int32_t norms;
+  int64_t T, d;
+  float eps;
+  float res_scale;
+  const void* X_out;
+  const void* Y;
+  const float* w_pre;
+  const float* w_post;
+  const float* gate_c;
+  const float* gate_t;
+  const void* dX_out;
+  const void* dN;
+  void* dX;
+  void* dY;
+  float* dw_pre;
+  float* dw_post;
+  float* dgate_c;
+  float* dgate_t;
+  void* workspace;
+  size_t workspace_bytes;
+} sfl_norm_bwd_args_t;
+
+/* Errors of both: SFL_E_ARG for bad sizes, unknown norm bits, eps below 0 or NaN, a NULL buffer
+ * that the call needs (T > 0) or one given that has no meaning (see above); SFL_E_UNSUPPORTED for
+ * d > 16384; SFL_E_WORKSPACE. T = 0 does nothing but clear the parameters' gradients. */
+sfl_status_t sfl_norm_forward(const sfl_norm_args_t* args, sfl_stream_t stream);
+sfl_status_t sfl_norm_backward(const sfl_norm_bwd_args_t* args, sfl_stream_t stream);
+
+/* Workspace bytes of sfl_norm_backward. */
+sfl_status_t sfl_norm_workspace_size(int64_t T, int64_t d, sfl_dtype_t dtype, size_t* bytes);
+
+/* Router: the k largest logits of each token and their softmax weights.
+ *  logits  [T][E] bf16 or fp32. An expert whose logit is -inf or NaN is not available.
+ *  expert  [T][k] int32: the chosen experts by descending logit, equal ones (+0 and -0 are) by
+ *          ascending index; -1 in the slots that are left where fewer than k are available
+ *  weight  [T][k] fp32: scale exp(l_j) / Z, Z the sum of exp over the chosen experts
+ *          (normalise = 1) or over all available ones (0); 0 where expert is -1. A logit of +inf
+ *          makes the token's weights NaN.
+ * 1 <= E <= 1024, 1 <= k <= 64, k <= E. Errors: SFL_E_ARG for bad sizes, normalise not 0/1 or a
+ * NULL buffer (T > 0); SFL_E_UNSUPPORTED for E > 1024, k > 64 or T > 2^31 - 1. */
+sfl_status_t sfl_route_forward(const void* logits, sfl_dtype_t dtype, int64_t T, int32_t E, int32_t k,
+                               int32_t normalise, float scale, int32_t* expert, float* weight, sfl_stream_t stream);
+
+/* Gradient of the weights with respect to the logits: dlogits [T][E] (dtype, overwritten) from
+ * dweight [T][k] and the forward's expert (as it wrote it). The choice is taken as constant; dweight
+ * is not read where expert is -1, and the logit of an expert that is not available gets 0. Errors
+ * as above. */
+sfl_status_t sfl_route_backward(const void* logits, sfl_dtype_t dtype, int64_t T, int32_t E, int32_t k,
+                                int32_t normalise, float scale, const int32_t* expert, const float* dweight,
+                                void* dlogits, sfl_stream_t stream);
+
+/* Tokens to their experts. Slot (t, j), the j-th choice of token t, gets a row of the expert order:
+ * rows are sorted by expert, an expert's rows by slot.
+ *  expert  [T][k] int32; a value outside [0, E) names no expert (the slot gets no row)
+ *  pos     [T][k] int32: the slot's row, or -1
+ *  offsets [E + 1] int32: the first row of each expert; offsets[E] is the number of rows
+ *  X, Xs   rows [T][d] and their copies in expert order, Xs[pos[t][j]] = X[t], Xs [rows][d]; both
+ *          NULL to make the order alone. A row beyond `rows` is not written, rows from offsets[E]
+ *          on are left as they are (rows = T k always suffices).
+ *  workspace  sfl_expert_workspace_size() bytes, 4-byte aligned (may be NULL when that is 0)
+ * 1 <= E <= 1024, 1 <= k <= 64. Errors: SFL_E_ARG for bad sizes, NULL buffers (T > 0; offsets
+ * always) or only one of X and Xs (Xs may be NULL with rows = 0); SFL_E_UNSUPPORTED for E > 1024,
+ * k > 64 or T k > 2^31 - 1; SFL_E_WORKSPACE. */
+sfl_status_t sfl_expert_dispatch(const int32_t* expert, int64_t T, int32_t k, int32_t E, int32_t* pos,
+                                 int32_t* offsets, const void* X, sfl_dtype_t dtype, int64_t d, int64_t rows, void* Xs,
+                                 void* workspace, size_t workspace_bytes, sfl_stream_t stream);
+sfl_status_t sfl_expert_workspace_size(int64_t T, int32_t k, int32_t E, size_t* bytes);
+
+/* The experts' rows back to their tokens: Y[t] = sum_j weight[t][j] Ys[pos[t][j]], summed in fp32
+ * by ascending j and rounded once. Slots with pos outside [0, rows) add nothing; a token without
+ * any gets zeros. weight [T][k] fp32 may be NULL for ones: with the gradient of Xs as Ys that is
+ * the gradient of sfl_expert_dispatch, dX. Ys [rows][d] and Y [T][d] do not overlap. Errors as
+ * above. */
+sfl_status_t sfl_expert_combine(const void* Ys, sfl_dtype_t dtype, int64_t T, int64_t d, int32_t k, const int32_t* pos,
+                                int64_t rows, const float* weight, void* Y, sfl_stream_t stream);
+
+/* Gradients of sfl_expert_combine: dYs[pos[t][j]] = weight[t][j] dY[t] (dYs [rows][d], rows that no
+ * slot names are left as they are) and dweight[t][j] = <dY[t], Ys[pos[t][j]]> (0 for a slot without
+ * a row). dYs or dweight may be NULL where it is not wanted, Ys then too where dweight is. dYs
+ * overlaps neither input. Errors as above. */
+sfl_status_t sfl_expert_combine_backward(const void* dY, const void* Ys, sfl_dtype_t dtype, int64_t T, int64_t d,
+                                         int32_t k, const int32_t* pos, int64_t rows, const float* weight, void* dYs,
+                                         float* dweight, sfl_stream_t stream);
+
+/* One tensor of a list of gradients (the list is host memory, read during the call only).
+ *  src    device pointer, n elements of dtype
+ *  dst    where sfl_grad_clip writes the scaled gradients; NULL or src: in place. Overlaps no
+ *         other tensor of the list. */
+typedef struct {
+  const void* src;
+  void* dst;
+  int64_t n;
+  int32_t dtype; /* sfl_dtype_t */
+  int32_t reserved;
+} sfl_grad_t;
+
+/* The sum of the squares of all elements of the list, fp64 [1] on the device (overwritten; 0 for an
+ * empty list). Formed in fp64: it neither overflows nor underflows for finite gradients. Ranks
+ * that hold parts of the gradients add their sums before they clip. workspace:
+ * sfl_grad_workspace_size() bytes, 8-byte aligned. Errors: SFL_E_ARG for n < 0, a NULL list (n > 0)
+ * or sumsq, an element count below 0, an unknown dtype or a NULL src with elements;
+ * SFL_E_WORKSPACE. */
+sfl_status_t sfl_grad_sumsq(const sfl_grad_t* list, int32_t n, double* sumsq, void* workspace, size_t workspace_bytes,
+                            sfl_stream_t stream);
+sfl_status_t sfl_grad_workspace_size(const sfl_grad_t* list, int32_t n, size_t* bytes);
+
+/* Clipping by the global norm: norm[0] (fp32, device, may be NULL) = sqrt(*sumsq), and every
+ * gradient times c = max_norm / norm where the norm is finite and above max_norm, else times 1
+ * (in place: left as it is). A norm that is not finite scales nothing: the caller sees it in norm
+ * and skips the step. max_norm >= 0, not NaN. Errors as above. */
+sfl_status_t sfl_grad_clip(const sfl_grad_t* list, int32_t n, const double* sumsq, float max_norm, float* norm,
+                           sfl_stream_t stream);
+
 /* Measurement utility (no step of the layer uses it): the bandwidth ceilings that the
  * kernels' rates are compared against, on the machine at hand.
  *  dst != NULL: copies bytes (rounded down to 16) from src to dst, reps times (the HBM copy

@@ -1,7 +1,8 @@
 """ctypes binding of libsfl (include/sfl.h). Argument marshalling only.
 
 Every function here has the name of the C entry point it calls and forwards
-device pointers (torch tensors' data_ptr()) and the current HIP stream. All
+device pointers (torch tensors' data_ptr()) and the current HIP stream; the operators
+around the layer also check the tensors' types, sizes and contiguity. All
 arithmetic happens in the HIP kernels of libsfl.so; if the library is missing
 or fails to load, importing this module raises (there is no fallback path).
 """
@@ -29,7 +30,10 @@ EXPORTED = ["sfl_status_string", "sfl_version", "sfl_twell_buffer_sizes", "sfl_p
             "sfl_workspace_size", "sfl_ffn_forward", "sfl_up_projection", "sfl_ffn_backward",
             "sfl_dense_ffn_baseline", "sfl_transpose", "sfl_pack_down_weights", "sfl_track_active_units",
             "sfl_reinit_dead_units", "sfl_ffn_forward_noalloc", "sfl_bandwidth_probe",
-            "sfl_down_projection_rowwise", "sfl_forward_workspace_size", "sfl_backward_workspace_size"]
+            "sfl_down_projection_rowwise", "sfl_forward_workspace_size", "sfl_backward_workspace_size",
+            "sfl_norm_forward", "sfl_norm_backward", "sfl_norm_workspace_size", "sfl_route_forward",
+            "sfl_route_backward", "sfl_expert_dispatch", "sfl_expert_workspace_size", "sfl_expert_combine",
+            "sfl_expert_combine_backward", "sfl_grad_sumsq", "sfl_grad_workspace_size", "sfl_grad_clip"]
 
 
 class SflError(RuntimeError):
@@ -78,6 +82,27 @@ class BwdArgs(Structure):
                 ("workspace", c_void_p), ("workspace_bytes", c_size_t), ("events", c_void_p), ("n_events", c_int32)]
 
 
+SFL_NORM_PRE, SFL_NORM_POST = 1, 2
+
+
+class NormArgs(Structure):
+    _fields_ = [("dtype", c_int), ("norms", c_int32), ("T", c_int64), ("d", c_int64), ("eps", ctypes.c_float),
+                ("res_scale", ctypes.c_float), ("X", c_void_p), ("Y", c_void_p), ("w_pre", c_void_p),
+                ("w_post", c_void_p), ("gate_c", c_void_p), ("gate_t", c_void_p), ("X_out", c_void_p), ("N", c_void_p)]
+
+
+class NormBwdArgs(Structure):
+    _fields_ = [("dtype", c_int), ("norms", c_int32), ("T", c_int64), ("d", c_int64), ("eps", ctypes.c_float),
+                ("res_scale", ctypes.c_float), ("X_out", c_void_p), ("Y", c_void_p), ("w_pre", c_void_p),
+                ("w_post", c_void_p), ("gate_c", c_void_p), ("gate_t", c_void_p), ("dX_out", c_void_p),
+                ("dN", c_void_p), ("dX", c_void_p), ("dY", c_void_p), ("dw_pre", c_void_p), ("dw_post", c_void_p),
+                ("dgate_c", c_void_p), ("dgate_t", c_void_p), ("workspace", c_void_p), ("workspace_bytes", c_size_t)]
+
+
+class Grad(Structure):
+    _fields_ = [("src", c_void_p), ("dst", c_void_p), ("n", c_int64), ("dtype", c_int32), ("reserved", c_int32)]
+
+
 _lib.sfl_status_string.restype = c_char_p
 _lib.sfl_status_string.argtypes = [c_int]
 _lib.sfl_version.restype = c_char_p
@@ -99,6 +124,23 @@ _lib.sfl_track_active_units.argtypes = [POINTER(Twell), c_int64, c_int64, c_int,
                                         c_void_p]
 _lib.sfl_reinit_dead_units.argtypes = [c_void_p, c_int, c_int64, c_int64, c_int32, c_void_p, c_int64, ctypes.c_float,
                                        ctypes.c_float, c_void_p, c_void_p]
+_lib.sfl_norm_forward.argtypes = [POINTER(NormArgs), c_void_p]
+_lib.sfl_norm_backward.argtypes = [POINTER(NormBwdArgs), c_void_p]
+_lib.sfl_norm_workspace_size.argtypes = [c_int64, c_int64, c_int, POINTER(c_size_t)]
+_lib.sfl_route_forward.argtypes = [c_void_p, c_int, c_int64, c_int32, c_int32, c_int32, ctypes.c_float, c_void_p,
+                                   c_void_p, c_void_p]
+_lib.sfl_route_backward.argtypes = [c_void_p, c_int, c_int64, c_int32, c_int32, c_int32, ctypes.c_float, c_void_p,
+                                    c_void_p, c_void_p, c_void_p]
+_lib.sfl_expert_dispatch.argtypes = [c_void_p, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int, c_int64,
+                                     c_int64, c_void_p, c_void_p, c_size_t, c_void_p]
+_lib.sfl_expert_workspace_size.argtypes = [c_int64, c_int32, c_int32, POINTER(c_size_t)]
+_lib.sfl_expert_combine.argtypes = [c_void_p, c_int, c_int64, c_int64, c_int32, c_void_p, c_int64, c_void_p, c_void_p,
+                                    c_void_p]
+_lib.sfl_expert_combine_backward.argtypes = [c_void_p, c_void_p, c_int, c_int64, c_int64, c_int32, c_void_p, c_int64,
+                                             c_void_p, c_void_p, c_void_p, c_void_p]
+_lib.sfl_grad_sumsq.argtypes = [POINTER(Grad), c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
+_lib.sfl_grad_workspace_size.argtypes = [POINTER(Grad), c_int32, POINTER(c_size_t)]
+_lib.sfl_grad_clip.argtypes = [POINTER(Grad), c_int32, c_void_p, ctypes.c_float, c_void_p, c_void_p]
 for _n in EXPORTED[2:]:
     getattr(_lib, _n).restype = c_int
 
@@ -322,6 +364,130 @@ def sfl_transpose(inp, out, stream=None):
     rows, cols = inp.shape
     _check("sfl_transpose", _lib.sfl_transpose(_ptr(inp), _ptr(out), rows, cols, inp.element_size(),
                                                _stream(stream)))
+
+
+# ---- around the layer: norms, router, experts, gradient clipping ----
+# These take the tensors themselves, so shapes, types and contiguity are checked here.
+_F32, _I32 = torch.float32, torch.int32
+
+
+def _buf(t, dtype, n):
+    """Device pointer of a contiguous tensor of n elements of dtype; None stays None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous {dtype} tensor of {n} elements, got {t.dtype} {tuple(t.shape)}"
+                         f"{'' if t.is_contiguous() else ' (not contiguous)'}")
+    return t.data_ptr()
+
+
+def _space(workspace):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def sfl_norm_forward(X, Y=None, *, X_out=None, N=None, norms=SFL_NORM_PRE | SFL_NORM_POST, w_pre=None, w_post=None,
+                     gate_c=None, gate_t=None, res_scale=1.0, eps=1e-6, stream=None):
+    T, d = X.shape
+    dt, n = X.dtype, T * d
+    a = NormArgs(dtype_code(dt), norms, T, d, eps, res_scale, _buf(X, dt, n), _buf(Y, dt, n), _buf(w_pre, _F32, d),
+                 _buf(w_post, _F32, d), _buf(gate_c, _F32, d), _buf(gate_t, _F32, T), _buf(X_out, dt, n),
+                 _buf(N, dt, n))
+    _check("sfl_norm_forward", _lib.sfl_norm_forward(a, _stream(stream)))
+
+
+def sfl_norm_workspace_size(T, d, dtype):
+    out = c_size_t(0)
+    _check("sfl_norm_workspace_size", _lib.sfl_norm_workspace_size(T, d, dtype_code(dtype), out))
+    return out.value
+
+
+def sfl_norm_backward(X_out, Y, dX_out, dN=None, *, dX=None, dY=None, dw_pre=None, dw_post=None, dgate_c=None,
+                      dgate_t=None, norms=SFL_NORM_PRE | SFL_NORM_POST, w_pre=None, w_post=None, gate_c=None,
+                      gate_t=None, res_scale=1.0, eps=1e-6, workspace=None, stream=None):
+    like = X_out if X_out is not None else dX_out
+    T, d = like.shape
+    dt, n = like.dtype, T * d
+    a = NormBwdArgs(dtype_code(dt), norms, T, d, eps, res_scale, _buf(X_out, dt, n), _buf(Y, dt, n),
+                    _buf(w_pre, _F32, d), _buf(w_post, _F32, d), _buf(gate_c, _F32, d), _buf(gate_t, _F32, T),
+                    _buf(dX_out, dt, n), _buf(dN, dt, n), _buf(dX, dt, n), _buf(dY, dt, n), _buf(dw_pre, _F32, d),
+                    _buf(dw_post, _F32, d), _buf(dgate_c, _F32, d), _buf(dgate_t, _F32, T), *_space(workspace))
+    _check("sfl_norm_backward", _lib.sfl_norm_backward(a, _stream(stream)))
+
+
+def sfl_route_forward(logits, expert, weight, *, normalise=True, scale=1.0, stream=None):
+    (T, E), k, dt = logits.shape, expert.shape[1], logits.dtype
+    _check("sfl_route_forward",
+           _lib.sfl_route_forward(_buf(logits, dt, T * E), dtype_code(dt), T, E, k, 1 if normalise else 0, scale,
+                                  _buf(expert, _I32, T * k), _buf(weight, _F32, T * k), _stream(stream)))
+
+
+def sfl_route_backward(logits, expert, dweight, dlogits, *, normalise=True, scale=1.0, stream=None):
+    (T, E), k, dt = logits.shape, expert.shape[1], logits.dtype
+    _check("sfl_route_backward",
+           _lib.sfl_route_backward(_buf(logits, dt, T * E), dtype_code(dt), T, E, k, 1 if normalise else 0, scale,
+                                   _buf(expert, _I32, T * k), _buf(dweight, _F32, T * k), _buf(dlogits, dt, T * E),
+                                   _stream(stream)))
+
+
+def sfl_expert_workspace_size(T, k, E):
+    out = c_size_t(0)
+    _check("sfl_expert_workspace_size", _lib.sfl_expert_workspace_size(T, k, E, out))
+    return out.value
+
+
+def sfl_expert_dispatch(expert, E, pos, offsets, *, X=None, Xs=None, workspace=None, stream=None):
+    T, k = expert.shape
+    n, dt, d, rows, px, ps = T * k, SFL_F32, 1, 0, None, None
+    if X is not None:
+        d, rows, dt = X.shape[1], Xs.shape[0], dtype_code(X.dtype)
+        px, ps = _buf(X, X.dtype, T * d), _buf(Xs, X.dtype, rows * d)
+    ws, ws_bytes = _space(workspace)
+    _check("sfl_expert_dispatch",
+           _lib.sfl_expert_dispatch(_buf(expert, _I32, n), T, k, E, _buf(pos, _I32, n), _buf(offsets, _I32, E + 1), px,
+                                    dt, d, rows, ps, ws, ws_bytes, _stream(stream)))
+
+
+def sfl_expert_combine(Ys, pos, Y, *, weight=None, stream=None):
+    (T, k), (rows, d), dt = pos.shape, Ys.shape, Ys.dtype
+    _check("sfl_expert_combine",
+           _lib.sfl_expert_combine(_buf(Ys, dt, rows * d), dtype_code(dt), T, d, k, _buf(pos, _I32, T * k), rows,
+                                   _buf(weight, _F32, T * k), _buf(Y, dt, T * d), _stream(stream)))
+
+
+def sfl_expert_combine_backward(dY, Ys, pos, weight, *, dYs=None, dweight=None, stream=None):
+    (T, k), d, dt = pos.shape, dY.shape[1], dY.dtype
+    rows = (dYs if Ys is None else Ys).shape[0]
+    _check("sfl_expert_combine_backward",
+           _lib.sfl_expert_combine_backward(_buf(dY, dt, T * d), _buf(Ys, dt, rows * d), dtype_code(dt), T, d, k,
+                                            _buf(pos, _I32, T * k), rows, _buf(weight, _F32, T * k),
+                                            _buf(dYs, dt, rows * d), _buf(dweight, _F32, T * k), _stream(stream)))
+
+
+def grad_list(grads, out=None):
+    """The list of gradients that the sfl_grad_* calls take; it keeps the tensors alive. out: where
+    the clipped gradients go, in place if None."""
+    a = (Grad * len(grads))()
+    a._keepalive = (grads, out)
+    for i, g in enumerate(grads):
+        dt, n = g.dtype, g.numel()
+        a[i] = (_buf(g, dt, n), None if out is None else _buf(out[i], dt, n), n, dtype_code(dt), 0)
+    return a
+
+
+def sfl_grad_workspace_size(grads):
+    out = c_size_t(0)
+    _check("sfl_grad_workspace_size", _lib.sfl_grad_workspace_size(grads, len(grads), out))
+    return out.value
+
+
+def sfl_grad_sumsq(grads, sumsq, *, workspace=None, stream=None):
+    _check("sfl_grad_sumsq", _lib.sfl_grad_sumsq(grads, len(grads), _buf(sumsq, torch.float64, 1), *_space(workspace),
+                                                 _stream(stream)))
+
+
+def sfl_grad_clip(grads, sumsq, max_norm, norm=None, *, stream=None):
+    _check("sfl_grad_clip", _lib.sfl_grad_clip(grads, len(grads), _buf(sumsq, torch.float64, 1), max_norm,
+                                               _buf(norm, _F32, 1), _stream(stream)))
 
 
 # ---- HIP events through the runtime library torch already loaded (for stage timing) ----

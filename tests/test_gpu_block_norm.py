@@ -1,0 +1,267 @@
+"""Block norms on the GPU against the float64 definition.
+
+Bounds: a row's mean squares and products are sums of d terms held in at least 64 partial sums, so
+d / 64 + 64 fp32 roundings cover a row's chain and what follows it; the parameters' gradients add
+T more. Rows stored in bf16 are rounded once."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block
+from tests.block_util import DT, Out, assert_rounded, f32, same_bits, shifted, stored
+
+pytestmark = pytest.mark.gpu
+
+b = pytest.importorskip("paper_2603_23198_amd.binding")
+
+SIZES = [(1, 1), (1, 64), (3, 7), (5, 257), (1, 2048), (4, 512), (9, 1003), (300, 96), (33, 4096), (3, 5000), (2, 8192),
+         (2, 8200), (2, 16384), (1500, 130)]
+FORMS = [dict(pre=True, post=True, gate_c=True, gate_t=True), dict(pre=True, post=True), dict(pre=True, post=False),
+         dict(pre=True, post=False, gate_c=True), dict(pre=False, post=True, gate_t=True),
+         dict(pre=True, post=False, no_y=True), dict(pre=False, post=False, gate_c=True, gate_t=True)]
+
+
+def setup(T, d, dt, form, seed, by=0):
+    r = np.random.default_rng(seed)
+    pre, post = form["pre"], form["post"]
+    dev, val = {}, {}
+
+    def put(name, a, kind):
+        if a is None:
+            dev[name] = val[name] = None
+            return
+        t, v = stored(a, kind)
+        dev[name], val[name] = (shifted(t, by) if by else t), v
+
+    put("X", 2 * r.standard_normal((T, d)), dt)
+    put("Y", None if form.get("no_y") else 1.5 * r.standard_normal((T, d)), dt)
+    put("dX_out", r.standard_normal((T, d)), dt)
+    put("dN", r.standard_normal((T, d)) if pre else None, dt)
+    put("w_pre", 1 + 0.1 * r.standard_normal(d) if pre and not form.get("ones") else None, "f32")
+    put("w_post", 1 + 0.1 * r.standard_normal(d) if post and not form.get("ones") else None, "f32")
+    put("gate_c", 0.5 + 0.3 * r.standard_normal(d) if form.get("gate_c") else None, "f32")
+    put("gate_t", r.uniform(-1, 1, T) if form.get("gate_t") else None, "f32")
+    norms = (b.SFL_NORM_PRE if pre else 0) | (b.SFL_NORM_POST if post else 0)
+    return dev, val, norms
+
+
+PARAMS = ("w_pre", "w_post", "gate_c", "gate_t")
+
+
+def forward(T, d, dt, form, seed=0, by=0, res_scale=0.75, eps=1e-6):
+    dev, val, norms = setup(T, d, dt, form, seed, by)
+    X_out, N = Out((T, d), DT[dt], by), Out((T, d), DT[dt], by) if form["pre"] else None
+    b.sfl_norm_forward(dev["X"], dev["Y"], X_out=X_out.t, N=N and N.t, norms=norms, res_scale=res_scale, eps=eps,
+                       **{n: dev[n] for n in PARAMS})
+    want, wn = block.norm_forward(val["X"], val["Y"], pre=form["pre"], post=form["post"], res_scale=res_scale, eps=eps,
+                                  **{n: val[n] for n in PARAMS})
+    terms = d / 64 + 64
+    assert_rounded(X_out.values(), *want, dt, terms, "X_out")
+    if N is not None:
+        assert_rounded(N.values(), *wn, dt, terms, "N")
+
+
+def backward(T, d, dt, form, seed=0, by=0, res_scale=0.75, eps=1e-6):
+    dev, val, norms = setup(T, d, dt, form, seed, by)
+    has_y = dev["Y"] is not None
+    outs = {"dX": Out((T, d), DT[dt], by)}
+    if has_y:
+        outs.update(dY=Out((T, d), DT[dt], by), dgate_c=Out((d,), torch.float32, by),
+                    dgate_t=Out((T,), torch.float32, by))
+    if form["pre"]:
+        outs["dw_pre"] = Out((d,), torch.float32, by)
+    if form["post"]:
+        outs["dw_post"] = Out((d,), torch.float32, by)
+    ws = torch.empty(b.sfl_norm_workspace_size(T, d, dt), dtype=torch.uint8, device="cuda")
+    b.sfl_norm_backward(dev["X"], dev["Y"], dev["dX_out"], dev["dN"], norms=norms, res_scale=res_scale, eps=eps,
+                        workspace=ws, **{n: dev[n] for n in PARAMS}, **{n: o.t for n, o in outs.items()})
+    want = block.norm_backward(val["X"], val["Y"], val["dX_out"], val["dN"], pre=form["pre"], post=form["post"],
+                               res_scale=res_scale, eps=eps, **{n: val[n] for n in PARAMS})
+    for n, o in outs.items():
+        rows = n in ("dX", "dY")
+        assert_rounded(o.values(), *want[n], dt if rows else "f32",
+                       d / 64 + 64 + (0 if rows or n == "dgate_t" else T), n)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d", SIZES)
+def test_forward(T, d, dt):
+    forward(T, d, dt, FORMS[0], seed=T + d)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d", SIZES)
+def test_backward(T, d, dt):
+    backward(T, d, dt, FORMS[0], seed=T + d)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("form", FORMS[1:] + [dict(pre=True, post=True, gate_c=True, ones=True)],
+                         ids=lambda f: "-".join(k for k, v in f.items() if v) or "none")
+def test_forms(form, dt):
+    for T, d in [(5, 264), (70, 1000), (3, 2048)]:
+        forward(T, d, dt, form, seed=d)
+        backward(T, d, dt, form, seed=d)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 1001, 2048])
+def test_element_alignment(d, dt):
+    for by in (1, 3):
+        forward(6, d, dt, FORMS[0], by=by)
+        backward(6, d, dt, FORMS[0], by=by)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_in_place_and_unwanted_outputs(dt):
+    T, d = 19, 520
+    dev, _, norms = setup(T, d, dt, FORMS[0], 3)
+    kw = dict(norms=norms, res_scale=0.5, **{n: dev[n] for n in PARAMS})
+    new = lambda: torch.empty_like(dev["X"])  # noqa: E731
+    X1, N1, X2, N2, N3 = new(), new(), dev["X"].clone(), new(), new()
+    b.sfl_norm_forward(dev["X"], dev["Y"], X_out=X1, N=N1, **kw)
+    b.sfl_norm_forward(X2, dev["Y"], X_out=X2, N=N2, **kw)
+    b.sfl_norm_forward(dev["X"], dev["Y"], N=N3, **kw)
+    assert same_bits(X1, X2) and same_bits(N1, N2) and same_bits(N1, N3)
+    ws = torch.empty(b.sfl_norm_workspace_size(T, d, dt), dtype=torch.uint8, device="cuda")
+    dX1, dY1, g1, dX2, dY3 = new(), new(), torch.empty(d, device="cuda"), dev["dX_out"].clone(), new()
+    b.sfl_norm_backward(X1, dev["Y"], dev["dX_out"], dev["dN"], dX=dX1, dY=dY1, dw_post=g1, workspace=ws, **kw)
+    b.sfl_norm_backward(X1, dev["Y"], dX2, dev["dN"], dX=dX2, workspace=ws, **kw)
+    b.sfl_norm_backward(X1, dev["Y"], dev["dX_out"], dev["dN"], dY=dY3, workspace=ws, **kw)
+    assert same_bits(dX1, dX2) and same_bits(dY1, dY3)
+    # a gradient that is not there is one of zeros
+    zero, a, c = torch.zeros_like(dev["X"]), new(), new()
+    b.sfl_norm_backward(X1, dev["Y"], None, dev["dN"], dX=a, workspace=ws, **kw)
+    b.sfl_norm_backward(X1, dev["Y"], zero, dev["dN"], dX=c, workspace=ws, **kw)
+    assert same_bits(a, c)
+    b.sfl_norm_backward(X1, dev["Y"], dev["dX_out"], None, dX=a, dY=dY1, workspace=ws, **kw)
+    b.sfl_norm_backward(X1, dev["Y"], dev["dX_out"], zero, dX=c, dY=dY3, workspace=ws, **kw)
+    assert torch.equal(a, c) and torch.equal(dY1, dY3)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [96, 1003, 4096])
+def test_zero_infinite_and_nan_rows_stay_to_themselves(d, dt):
+    T = 12
+    dev, _, norms = setup(T, d, dt, FORMS[0], 5)
+    kw = dict(norms=norms, **{n: dev[n] for n in PARAMS})
+    X_out, N = torch.empty_like(dev["X"]), torch.empty_like(dev["X"])
+    b.sfl_norm_forward(dev["X"], dev["Y"], X_out=X_out, N=N, **kw)
+    X, Y = dev["X"].clone(), dev["Y"].clone()
+    X[1], Y[1] = 0, 0                      # a row of zeros: the norms' eps keeps it finite
+    Y[4, d // 2], X[7, 0] = float("inf"), float("nan")
+    X2, N2 = torch.empty_like(X), torch.empty_like(X)
+    b.sfl_norm_forward(X, Y, X_out=X2, N=N2, **kw)
+    keep = [t for t in range(T) if t not in (1, 4, 7)]
+    assert same_bits(X2[keep], X_out[keep]) and same_bits(N2[keep], N[keep])
+    assert (X2[1] == 0).all() and (N2[1] == 0).all()
+    assert N2[4].isnan().any() and N2[7].isnan().all()
+    ws = torch.empty(b.sfl_norm_workspace_size(T, d, dt), dtype=torch.uint8, device="cuda")
+    out = {n: torch.empty_like(X) for n in ("dX", "dY")}
+    b.sfl_norm_backward(X_out, dev["Y"], dev["dX_out"], dev["dN"], workspace=ws, **out, **kw)
+    X_out2 = X_out.clone()
+    X_out2[1] = 0
+    out2 = {n: torch.empty_like(X) for n in ("dX", "dY")}
+    b.sfl_norm_backward(X_out2, Y, dev["dX_out"], dev["dN"], workspace=ws, **out2, **kw)
+    keep = [t for t in range(T) if t not in (1, 4)]
+    for n in out:
+        assert same_bits(out2[n][keep], out[n][keep])
+        assert out2[n][1].isfinite().all()
+
+
+def test_no_rows_clear_the_parameter_gradients():
+    d = 300
+    e = torch.empty((0, d), dtype=torch.bfloat16, device="cuda")
+    g = {n: torch.full((d,), 5.0, device="cuda") for n in ("dw_pre", "dw_post", "dgate_c")}
+    b.sfl_norm_forward(e, e, X_out=e, N=e)
+    b.sfl_norm_backward(e, e, e, e, dX=e, dY=e, **g)
+    assert all((t == 0).all() for t in g.values())
+
+
+@pytest.mark.parametrize("T,d", [(3000, 136), (700, 4096)])
+def test_results_are_the_same_from_call_to_call(T, d):
+    dev, _, norms = setup(T, d, "bf16", FORMS[0], 9)
+    ws = torch.empty(b.sfl_norm_workspace_size(T, d, "bf16"), dtype=torch.uint8, device="cuda")
+    runs = []
+    for _ in range(2):
+        o = {n: torch.empty_like(dev["X"]) for n in ("dX", "dY")}
+        o.update({n: torch.empty(d, device="cuda") for n in ("dw_pre", "dw_post", "dgate_c")})
+        ws.fill_(0xA5)
+        b.sfl_norm_backward(dev["X"], dev["Y"], dev["dX_out"], dev["dN"], norms=norms, workspace=ws, **o,
+                            **{n: dev[n] for n in PARAMS})
+        runs.append(o)
+    assert all(same_bits(runs[0][n], runs[1][n]) for n in runs[0])
+
+
+def test_gradient_against_differences():
+    """The fp32 gradient along a random direction against central differences of the float64
+    forward. Both directional derivatives are sums over T d terms; with h = 1e-4 the difference
+    quotient's own error is about h^2 = 1e-8 of the third derivative's scale."""
+    T, d = 6, 200
+    dev, val, norms = setup(T, d, "f32", FORMS[0], 13)
+    kw = dict(norms=norms, res_scale=0.75, eps=1e-3)
+    X_out, N = torch.empty_like(dev["X"]), torch.empty_like(dev["X"])
+    b.sfl_norm_forward(dev["X"], dev["Y"], X_out=X_out, N=N, **kw, **{n: dev[n] for n in PARAMS})
+    g = {n: torch.empty_like(dev["X"]) for n in ("dX", "dY")}
+    g.update({"d" + n: torch.empty_like(dev[n]) for n in PARAMS})
+    ws = torch.empty(b.sfl_norm_workspace_size(T, d, "f32"), dtype=torch.uint8, device="cuda")
+    b.sfl_norm_backward(X_out, dev["Y"], dev["dX_out"], dev["dN"], workspace=ws, **g, **kw,
+                        **{n: dev[n] for n in PARAMS})
+
+    def f(v):
+        (Xo, _), (n, _) = block.norm_forward(v["X"], v["Y"], pre=True, post=True, res_scale=0.75, eps=1e-3,
+                                             **{n: v[n] for n in PARAMS})
+        return (val["dX_out"] * Xo).sum() + (val["dN"] * n).sum()
+
+    r, h = np.random.default_rng(17), 1e-4
+    for name in ("X", "Y") + PARAMS:
+        v = r.standard_normal(val[name].shape)
+        up, down = dict(val), dict(val)
+        up[name], down[name] = val[name] + h * v, val[name] - h * v
+        quotient = (f(up) - f(down)) / (2 * h)
+        terms = g["d" + name].cpu().double().numpy() * v
+        assert abs(quotient - terms.sum()) <= 1e-5 * np.abs(terms).sum(), name
+
+
+def test_rows_beyond_32_bit_offsets():
+    T, d = (1 << 31) // 16384 + 5, 16384
+    dev = "cuda"
+    X = torch.zeros((T, d), dtype=torch.bfloat16, device=dev)
+    Y, N = torch.zeros_like(X), torch.empty_like(X)
+    g = torch.Generator(device=dev)
+    g.manual_seed(3)
+    X[-3:] = torch.randn((3, d), generator=g, device=dev).bfloat16()
+    Y[-3:] = torch.randn((3, d), generator=g, device=dev).bfloat16()
+    small, sn = torch.empty((3, d), dtype=torch.bfloat16, device=dev), torch.empty((3, d), dtype=torch.bfloat16, device=dev)
+    b.sfl_norm_forward(X[-3:], Y[-3:], X_out=small, N=sn)
+    dXs, dYs = torch.empty_like(small), torch.empty_like(small)
+    ws = torch.empty(b.sfl_norm_workspace_size(T, d, "bf16"), dtype=torch.uint8, device=dev)
+    b.sfl_norm_backward(small, Y[-3:], X[-3:], sn, dX=dXs, dY=dYs, workspace=ws)
+    b.sfl_norm_forward(X, Y, X_out=X, N=N)
+    assert same_bits(X[-3:], small) and same_bits(N[-3:], sn)
+    assert not N[:5].any() and not X[T // 2].any()
+    X[-3:] = small
+    dX = torch.zeros_like(X)
+    dX[-3:] = torch.randn((3, d), generator=g, device=dev).bfloat16()
+    dXs2, dYs2 = torch.empty_like(small), torch.empty_like(small)
+    b.sfl_norm_backward(small, Y[-3:], dX[-3:], sn, dX=dXs2, dY=dYs2, workspace=ws)
+    dY = torch.empty_like(X)
+    b.sfl_norm_backward(X, Y, dX, N, dX=dX, dY=dY, workspace=ws)
+    assert torch.equal(dX[-3:], dXs2) and torch.equal(dY[-3:], dYs2)
+
+
+def test_on_another_stream():
+    T, d = 64, 1024
+    dev, _, norms = setup(T, d, "bf16", FORMS[0], 21)
+    want, got, N = (torch.empty_like(dev["X"]) for _ in range(3))
+    kw = dict(norms=norms, **{n: dev[n] for n in PARAMS})
+    b.sfl_norm_forward(dev["X"], dev["Y"], X_out=want, N=N, **kw)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    late = torch.empty_like(dev["Y"])
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(2_000_000)
+        late.copy_(dev["Y"])
+        b.sfl_norm_forward(dev["X"], late, X_out=got, N=N, **kw)
+    side.synchronize()
+    assert same_bits(want, got)
