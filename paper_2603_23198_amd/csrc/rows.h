@@ -1,0 +1,91 @@
+// Row access shared by the operators around the layer: eight consecutive elements of a row per
+// thread, whatever the row's alignment, and sums over the threads of a row.
+#pragma once
+
+#include "common.h"
+
+namespace sfl {
+
+constexpr int kVec = 8;  // elements of one load: 16 bytes of bf16, two times 16 of fp32
+
+// Eight elements as loaded (bf16 stays packed until it is used).
+template <typename V> struct Vec8;
+template <> struct Vec8<bf16_t> {
+  u32x4_t w;
+  __device__ __forceinline__ float get(int i) const { return i & 1 ? bf16hi(w[i / 2]) : bf16lo(w[i / 2]); }
+};
+template <> struct Vec8<float> {
+  f32x4_t a, b;
+  __device__ __forceinline__ float get(int i) const { return i < 4 ? a[i] : b[i - 4]; }
+};
+
+// 16 bytes at an address of element alignment: one load or store (the memory system takes
+// unaligned vector accesses).
+template <typename T, typename P> __device__ __forceinline__ T load16(const P* p) {
+  T v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+template <typename T, typename P> __device__ __forceinline__ void store16(P* p, T v) { __builtin_memcpy(p, &v, 16); }
+
+__device__ __forceinline__ Vec8<bf16_t> load_full(const bf16_t* p) { return {load16<u32x4_t>(p)}; }
+__device__ __forceinline__ Vec8<float> load_full(const float* p) { return {load16<f32x4_t>(p), load16<f32x4_t>(p + 4)}; }
+
+// Elements c .. c + 7 of a row of d; zeros past its end.
+template <typename V> __device__ __forceinline__ Vec8<V> load8(const V* row, int c, int d) {
+  if (c + kVec <= d) return load_full(row + c);
+  Vec8<V> v{};
+  if (c < d) {
+    V e[kVec] = {};
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      if (c + i < d) e[i] = row[c + i];
+    __builtin_memcpy(&v, e, sizeof(e));
+  }
+  return v;
+}
+
+// Two floats to packed bf16, each to nearest even (NaN stays a NaN).
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  return (uint32_t)f32_to_bf16(lo) | (uint32_t)f32_to_bf16(hi) << 16;
+}
+
+template <typename V> __device__ __forceinline__ void store8(V* row, int c, int d, const float (&v)[kVec]);
+template <> __device__ __forceinline__ void store8<bf16_t>(bf16_t* row, int c, int d, const float (&v)[kVec]) {
+  if (c + kVec <= d) {
+    store16(row + c, u32x4_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])});
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      if (c + i < d) row[c + i] = f32_to_bf16(v[i]);
+  }
+}
+template <> __device__ __forceinline__ void store8<float>(float* row, int c, int d, const float (&v)[kVec]) {
+  if (c + kVec <= d) {
+    store16(row + c, f32x4_t{v[0], v[1], v[2], v[3]});
+    store16(row + c + 4, f32x4_t{v[4], v[5], v[6], v[7]});
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      if (c + i < d) row[c + i] = v[i];
+  }
+}
+
+template <int CTRL> __device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+
+// Sum over aligned groups of N <= 64 lanes, in every lane. Lanes trade inside a row of 16 by DPP
+// (no LDS round trip); the four rows of a wave are read out and added in lane order.
+template <int N> __device__ __forceinline__ float group_sum(float v) {
+  static_assert(N >= 2 && N <= 64 && (N & (N - 1)) == 0, "");
+  v = dpp_add<0xB1>(v);               // quad_perm: lane ^ 1
+  if (N >= 4) v = dpp_add<0x4E>(v);   // quad_perm: lane ^ 2
+  if (N >= 8) v = dpp_add<0x141>(v);  // row_half_mirror: the other quad of eight lanes
+  if (N >= 16) v = dpp_add<0x140>(v);  // row_mirror: the other eight of the row
+  if (N == 32) v += __shfl_xor(v, 16, 64);
+  if (N == 64) v = (readlane_f(v, 0) + readlane_f(v, 16)) + (readlane_f(v, 32) + readlane_f(v, 48));
+  return v;
+}
+
+}  // namespace sfl
