@@ -569,7 +569,7 @@ sfl_status_t sfl_route_backward(const void* logits, sfl_dtype_t dtype, int64_t T
  *  workspace  sfl_expert_workspace_size() bytes, 4-byte aligned (may be NULL when that is 0)
  * 1 <= E <= 1024, 1 <= k <= 64. Errors: SFL_E_ARG for bad sizes, NULL buffers (T > 0; offsets
  * always) or only one of X and Xs (Xs may be NULL with rows = 0); SFL_E_UNSUPPORTED for E > 1024,
- * k > 64 or T k > 2^31 - 1; SFL_E_WORKSPACE. */
+ * k > 64, T k > 2^31 - 1 or d > 2^30; SFL_E_WORKSPACE. */
 sfl_status_t sfl_expert_dispatch(const int32_t* expert, int64_t T, int32_t k, int32_t E, int32_t* pos,
                                  int32_t* offsets, const void* X, sfl_dtype_t dtype, int64_t d, int64_t rows, void* Xs,
                                  void* workspace, size_t workspace_bytes, sfl_stream_t stream);

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from ctypes import POINTER, Structure, c_char_p, c_double, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
@@ -466,11 +467,12 @@ def sfl_expert_combine_backward(dY, Ys, pos, weight, *, dYs=None, dweight=None, 
 def grad_list(grads, out=None):
     """The list of gradients that the sfl_grad_* calls take; it keeps the tensors alive. out: where
     the clipped gradients go, in place if None."""
-    a = (Grad * len(grads))()
-    a._keepalive = (grads, out)
+    rows = array("q")  # Grad's fields, 8 bytes each (dtype and reserved together)
     for i, g in enumerate(grads):
         dt, n = g.dtype, g.numel()
-        a[i] = (_buf(g, dt, n), None if out is None else _buf(out[i], dt, n), n, dtype_code(dt), 0)
+        rows.extend((_buf(g, dt, n) or 0, 0 if out is None else _buf(out[i], dt, n) or 0, n, dtype_code(dt)))
+    a = (Grad * len(grads)).from_buffer(rows) if rows else (Grad * 0)()
+    a._keepalive = (grads, out)
     return a
 
 

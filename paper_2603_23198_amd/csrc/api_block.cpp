@@ -45,7 +45,8 @@ sfl_status_t check_slots(int64_t T, int32_t k) {
 sfl_status_t check_rows(sfl_dtype_t dtype, int64_t T, int64_t d, int32_t k, int64_t rows) {
   const sfl_status_t st = check_slots(T, k);
   if (st != SFL_OK) return st;
-  return dtype_ok(dtype) && size_ok(T, d) && size_ok(rows, d) ? SFL_OK : SFL_E_ARG;
+  if (!dtype_ok(dtype) || !size_ok(T, d) || !size_ok(rows, d)) return SFL_E_ARG;
+  return d > ((int64_t)1 << 30) ? SFL_E_UNSUPPORTED : SFL_OK;
 }
 
 sfl_status_t check_grads(const sfl_grad_t* list, int32_t n) {
@@ -168,10 +169,8 @@ sfl_status_t sfl_expert_dispatch(const int32_t* expert, int64_t T, int32_t k, in
   if (T > 0 && (!expert || !pos || (X && !Xs && rows > 0) || (Xs && !X))) return SFL_E_ARG;
   const size_t need = expert_workspace_bytes(T, k, E);
   if (need > 0 && (!workspace || workspace_bytes < need)) return SFL_E_WORKSPACE;
-  hipError_t e = launch_expert_order(expert, T, k, E, pos, offsets, workspace, (hipStream_t)stream);
-  if (e == hipSuccess && X)
-    e = launch_expert_rows(X, dtype == SFL_BF16, T, d, k, pos, rows, Xs, (hipStream_t)stream);
-  return status(e);
+  return status(launch_expert_dispatch(expert, T, k, E, pos, offsets, X, dtype == SFL_BF16, d, rows, Xs, workspace,
+                                       (hipStream_t)stream));
 }
 
 sfl_status_t sfl_expert_combine(const void* Ys, sfl_dtype_t dtype, int64_t T, int64_t d, int32_t k, const int32_t* pos,

@@ -61,12 +61,11 @@ hipError_t launch_route_bwd(const void* logits, int bf16, int64_t T, int E, int 
 // -------------------------------------------------------------------------- experts ----
 size_t expert_workspace_bytes(int64_t T, int k, int E);
 // pos[t k + j] = row of slot (t, j) in expert order (stable), -1 for an expert outside
-// [0, E); offsets[e] = first row of expert e, offsets[E] = number of rows.
-hipError_t launch_expert_order(const int32_t* expert, int64_t T, int k, int E, int32_t* pos, int32_t* offsets,
-                               void* workspace, hipStream_t s);
-// Xs[pos[t k + j]] = X[t]
-hipError_t launch_expert_rows(const void* X, int bf16, int64_t T, int64_t d, int k, const int32_t* pos, int64_t rows,
-                              void* Xs, hipStream_t s);
+// [0, E); offsets[e] = first row of expert e, offsets[E] = number of rows; and, where X is not
+// null, Xs[pos[t k + j]] = X[t].
+hipError_t launch_expert_dispatch(const int32_t* expert, int64_t T, int k, int E, int32_t* pos, int32_t* offsets,
+                                  const void* X, int bf16, int64_t d, int64_t rows, void* Xs, void* workspace,
+                                  hipStream_t s);
 // Y[t] = sum_j w[t k + j] Ys[pos[t k + j]]
 hipError_t launch_expert_combine(const void* Ys, int bf16, int64_t T, int64_t d, int k, const int32_t* pos,
                                  int64_t rows, const float* weight, void* Y, hipStream_t s);

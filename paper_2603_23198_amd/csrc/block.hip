@@ -263,9 +263,10 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_bwd(NormBwdParams p
   }
 }
 
-// Parameter gradients from the workgroups' sums: a workgroup takes 64 columns of one of the two,
-// its threads 16 groups of rows, added in a fixed order.
-constexpr int kSumCols = 64, kSumThreads = 1024;
+// Parameter gradients from the workgroups' sums: a workgroup takes 32 columns of one of the two,
+// its threads 32 groups of rows, added in a fixed order (64 columns: 7.0 us at d = 4096 for 128
+// workgroups).
+constexpr int kSumCols = 32, kSumThreads = 1024;
 __global__ __launch_bounds__(kSumThreads) void k_norm_param_sums(NormBwdParams p, int blocks) {
   __shared__ float red[kSumThreads / kSumCols][kSumCols];
   const int64_t cols = cdiv(p.d, kSumCols);
@@ -331,7 +332,9 @@ hipError_t launch_norm_fwd(const NormParams& p, int bf16, hipStream_t s) {
   return with_layout(p.d, [&](auto nt, auto ch) {
     constexpr int NT = decltype(nt)::value, CH = decltype(ch)::value;
     using L = Rows<NT>;
-    const unsigned grid = (unsigned)std::min<int64_t>(cdiv(p.T, L::R), 256 * (2048 / L::kThreads));
+    // twice what the chip holds at a time: rows of a second round fill in where the first's end
+    // (8192 x 4096 bf16: 60 us with one round, 56 with two, 64 with a workgroup per row)
+    const unsigned grid = (unsigned)std::min<int64_t>(cdiv(p.T, L::R), 256 * (4096 / L::kThreads));
     if (bf16)
       hipLaunchKernelGGL((k_norm_fwd<bf16_t, NT, CH>), dim3(grid), dim3(L::kThreads), 0, s, p);
     else

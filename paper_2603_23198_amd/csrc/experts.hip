@@ -3,10 +3,13 @@
 //   pos(s) = #{slots of lower experts} + #{earlier slots of the same expert}, -1 for a slot of
 //   no expert; Xs[pos] = X[t]; Y[t] = sum_j w Ys[pos]; dYs[pos] = w dY[t]; dw = <dY[t], Ys[pos]>.
 // The gradient of the way there, dX[t] = sum_j dXs[pos], is the way back with weights of one.
-// Every pass walks the tokens, so a token's row is read or written once however many experts it
-// has. Sums run over j in order, in fp32: results do not depend on any other token.
+//
+// The passes over the rows are bound by memory and walk the tokens, so a token's own row is read
+// or written once however many experts it has; the expert side's rows (1 + k or 1 + 2 k rows of
+// traffic per token in all) are whole contiguous rows wherever they lie. Sums run over j in order,
+// in fp32, and no sum depends on another token: there are no atomics.
 #include "block.h"
-#include "common.h"
+#include "rows.h"
 
 #include <algorithm>
 
@@ -17,42 +20,159 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kOrderThreads = 1024;
 
-// One workgroup sorts all slots, 1024 at a time in slot order. LDS: next[E], the next free row
-// of each expert, and tile[waves][E], the current tile's slots of each wave and expert.
-__global__ __launch_bounds__(kOrderThreads) void k_expert_order(const int32_t* __restrict__ expert, int64_t n, int E,
+// ------------------------------------------------------------------------- the order ----
+
+__device__ __forceinline__ int valid_expert(int e, int E) { return e >= 0 && e < E ? e : -1; }
+
+// Exclusive prefix sums of total[E] in place by the first wave's lanes (a run of E / 64 each);
+// returns the sum of all to every lane of that wave.
+__device__ __forceinline__ int scan_experts(int* total, int E) {
+  const int lane = lane_id(), run = (E + kWave - 1) / kWave, e0 = min(lane * run, E), e1 = min(e0 + run, E);
+  int s = 0;
+  for (int e = e0; e < e1; ++e) s += total[e];
+  const int incl = wave_incl_scan(s);
+  s = incl - s;
+  for (int e = e0; e < e1; ++e) {
+    const int c = total[e];
+    total[e] = s;
+    s += c;
+  }
+  return readlane_i(incl, kWave - 1);
+}
+
+// Counts of a workgroup's slots [first, last) per expert.
+__device__ __forceinline__ void count_experts(const int32_t* __restrict__ expert, int64_t first, int64_t last, int E,
+                                              int* cnt, int threads) {
+  for (int e = threadIdx.x; e < E; e += threads) cnt[e] = 0;
+  __syncthreads();
+  for (int64_t i = first + threadIdx.x; i < last; i += threads) {
+    const int e = expert[i];
+    if (e >= 0 && e < E) atomicAdd(&cnt[e], 1);
+  }
+  __syncthreads();
+}
+
+// Few slots: workgroup t finds the rows of token t's slots by counting over all slots, and copies
+// the token's row to them; one more workgroup writes the offsets. Every thread holds up to
+// kSmallPer slots; a wave's count is a ballot per 64 slots.
+constexpr int kSmallPer = 16, kSmallSlots = kSmallPer * kThreads;
+
+template <typename V>
+__global__ __launch_bounds__(kThreads) void k_expert_small(const int32_t* __restrict__ expert, int n, int k, int E,
+                                                           int32_t* __restrict__ pos, int32_t* __restrict__ offsets,
+                                                           const V* __restrict__ X, int64_t d, int64_t rows,
+                                                           V* __restrict__ Xs) {
+  __shared__ int cnt[kRouteMaxExperts];  // the offsets' workgroup; [k][4] partial counts in the others
+  const int64_t t = blockIdx.x;
+  if (t == gridDim.x - 1) {
+    count_experts(expert, 0, n, E, cnt, kThreads);
+    if (threadIdx.x < kWave) {
+      const int sum = scan_experts(cnt, E);
+      if (threadIdx.x == 0) offsets[E] = sum;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += kThreads) offsets[e] = cnt[e];
+    return;
+  }
+  constexpr int W = kThreads / kWave;
+  const int wave = threadIdx.x / kWave;
+  int mine[kSmallPer];
+#pragma unroll
+  for (int i = 0; i < kSmallPer; ++i) {
+    const int s = i * kThreads + threadIdx.x;
+    mine[i] = s < n ? valid_expert(expert[s], E) : -1;
+  }
+  for (int j = 0; j < k; ++j) {
+    const int s = (int)t * k + j, e = valid_expert(expert[s], E);
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < kSmallPer; ++i)
+      if (i * kThreads < n)
+        before += __popcll(ballot(mine[i] >= 0 && (mine[i] < e || (mine[i] == e && i * kThreads + (int)threadIdx.x < s))));
+    if (lane_id() == 0) cnt[j * W + wave] = before;
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < k) {
+    const int s = (int)t * k + threadIdx.x, e = valid_expert(expert[s], E);
+    int p = -1;
+    if (e >= 0) {
+      p = 0;
+#pragma unroll
+      for (int w = 0; w < W; ++w) p += cnt[threadIdx.x * W + w];
+    }
+    pos[s] = p;
+    cnt[kRouteMaxK * W + threadIdx.x] = p;
+  }
+  if (!X) return;
+  __syncthreads();
+  const V* from = X + t * d;
+  for (int64_t c = (int64_t)threadIdx.x * kVec; c < d; c += kThreads * kVec) {
+    const Vec8<V> v = load8(from, (int)c, (int)d);
+    for (int j = 0; j < k; ++j) {
+      const int p = cnt[kRouteMaxK * W + j];
+      if (p >= 0 && p < rows) copy8(Xs + p * d, (int)c, (int)d, v);
+    }
+  }
+}
+
+// Many slots: each workgroup takes a run of slots, counts its experts, and in a second launch adds
+// up the counts before it and places its slots.
+__global__ __launch_bounds__(kOrderThreads) void k_expert_count(const int32_t* __restrict__ expert, int64_t n,
+                                                                int64_t run, int E, int32_t* __restrict__ count) {
+  extern __shared__ int lds[];
+  const int64_t first = blockIdx.x * run;
+  count_experts(expert, first, min(first + run, n), E, lds, kOrderThreads);
+  for (int e = threadIdx.x; e < E; e += kOrderThreads) count[(int64_t)blockIdx.x * E + e] = lds[e];
+}
+
+// LDS: total[E], next[E] (the next free row of each expert) and tile[waves][E] (the current 1024
+// slots of each wave and expert).
+__global__ __launch_bounds__(kOrderThreads) void k_expert_place(const int32_t* __restrict__ expert, int64_t n,
+                                                                int64_t run, int E, const int32_t* __restrict__ count,
                                                                 int32_t* __restrict__ pos,
                                                                 int32_t* __restrict__ offsets) {
-  extern __shared__ int32_t lds[];
-  int32_t* next = lds;
-  int32_t* tile = lds + E;
-  const int waves = kOrderThreads / kWave, wave = threadIdx.x / kWave;
-  for (int e = threadIdx.x; e < E; e += kOrderThreads) next[e] = 0;
+  extern __shared__ int lds[];
+  constexpr int W = kOrderThreads / kWave;
+  int* total = lds;
+  int* next = lds + E;
+  int* tile = lds + 2 * E;
+  const int wave = threadIdx.x / kWave;
+  // sums over the workgroups before this one and over all, 1024 / E' parts of them at a time
+  int width = 1;
+  while (width < E) width *= 2;
+  const int parts = kOrderThreads / width, part = threadIdx.x / width, e0 = threadIdx.x % width;
+  for (int e = threadIdx.x; e < E; e += kOrderThreads) total[e] = next[e] = 0;
   __syncthreads();
-  for (int64_t i = threadIdx.x; i < n; i += kOrderThreads) {
-    const int e = expert[i];
-    if (e >= 0 && e < E) atomicAdd(&next[e], 1);
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    int sum = 0;
-    for (int e = 0; e < E; ++e) {
-      const int c = next[e];
-      next[e] = sum;
-      offsets[e] = sum;
-      sum += c;
+  if (e0 < E) {
+    int all = 0, before = 0;
+    for (int b = part; b < (int)gridDim.x; b += parts) {
+      const int c = count[(int64_t)b * E + e0];
+      all += c;
+      before += b < (int)blockIdx.x ? c : 0;
     }
-    offsets[E] = sum;
+    atomicAdd(&total[e0], all);  // whole numbers: their order does not matter
+    atomicAdd(&next[e0], before);
   }
-  for (int64_t i0 = 0; i0 < n; i0 += kOrderThreads) {
-    for (int e = threadIdx.x; e < waves * E; e += kOrderThreads) tile[e] = 0;
+  __syncthreads();
+  if (wave == 0) {
+    const int sum = scan_experts(total, E);
+    if (blockIdx.x == 0 && threadIdx.x == 0) offsets[E] = sum;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < E; e += kOrderThreads) {
+    if (blockIdx.x == 0) offsets[e] = total[e];
+    next[e] += total[e];
+  }
+  const int64_t first = blockIdx.x * run, last = min(first + run, n);
+  for (int64_t i0 = first; i0 < last; i0 += kOrderThreads) {
+    for (int e = threadIdx.x; e < W * E; e += kOrderThreads) tile[e] = 0;
     __syncthreads();
     const int64_t i = i0 + threadIdx.x;
-    int e = i < n ? expert[i] : -1;
-    if (e >= E) e = -1;
+    const int e = i < last ? valid_expert(expert[i], E) : -1;
     // lanes of this wave with the same expert
-    uint64_t same = __ballot(e >= 0);
+    uint64_t same = ballot(e >= 0);
     for (int b = 0; (1 << b) < E; ++b) {
-      const uint64_t m = __ballot((e >> b) & 1);
+      const uint64_t m = ballot((e >> b) & 1);
       same &= ((e >> b) & 1) ? m : ~m;
     }
     const int before = mbcnt(same);
@@ -62,124 +182,230 @@ __global__ __launch_bounds__(kOrderThreads) void k_expert_order(const int32_t* _
       int row = next[e] + before;
       for (int w = 0; w < wave; ++w) row += tile[w * E + e];
       pos[i] = row;
-    } else if (i < n) {
+    } else if (i < last) {
       pos[i] = -1;
     }
+    if (i0 + kOrderThreads >= last) break;
     __syncthreads();
-    for (int x = threadIdx.x; x < E; x += kOrderThreads)
-      for (int w = 0; w < waves; ++w) next[x] += tile[w * E + x];
+    for (int x = threadIdx.x; x < E; x += kOrderThreads) {
+      int c = 0;
+      for (int w = 0; w < W; ++w) c += tile[w * E + x];
+      next[x] += c;
+    }
     __syncthreads();
   }
 }
 
-template <typename V>
-__global__ __launch_bounds__(kThreads) void k_expert_rows(const V* __restrict__ X, int64_t T, int64_t d, int k,
+// Slots of a workgroup: a tile of 1024, more where that would take over 256 workgroups (each adds
+// up the others' counts).
+int64_t order_run(int64_t n) { return cdiv(cdiv(n, 256), kOrderThreads) * kOrderThreads; }
+
+// -------------------------------------------------------------------------- the rows ----
+// NT threads per token, chunk after chunk of 8 columns each; R tokens per workgroup.
+
+template <typename V, int NT>
+__global__ __launch_bounds__(kThreads) void k_expert_rows(const V* __restrict__ X, int64_t T, int64_t d64, int k,
                                                           const int32_t* __restrict__ pos, int64_t rows,
                                                           V* __restrict__ Xs) {
-  for (int64_t t = blockIdx.x; t < T; t += gridDim.x)
-    for (int64_t c = threadIdx.x; c < d; c += kThreads) {
-      const V v = X[t * d + c];
-      for (int j = 0; j < k; ++j) {
-        const int p = pos[t * k + j];
-        if (p >= 0 && p < rows) Xs[p * d + c] = v;
-      }
+  const int64_t t = (int64_t)blockIdx.x * (kThreads / NT) + threadIdx.x / NT;
+  if (t >= T) return;
+  const int d = (int)d64;
+  const V* from = X + t * d64;
+  for (int c = threadIdx.x % NT * kVec; c < d; c += NT * kVec) {
+    const Vec8<V> v = load8(from, c, d);
+    for (int j = 0; j < k; ++j) {
+      const int p = pos[t * k + j];
+      if (p >= 0 && p < rows) copy8(Xs + p * d64, c, d, v);
     }
+  }
 }
 
-template <typename V>
-__global__ __launch_bounds__(kThreads) void k_expert_combine(const V* __restrict__ Ys, int64_t T, int64_t d, int k,
+constexpr int kSlots = 4;  // slots whose rows are in flight together
+
+template <typename V, int NT>
+__global__ __launch_bounds__(kThreads) void k_expert_combine(const V* __restrict__ Ys, int64_t T, int64_t d64, int k,
                                                              const int32_t* __restrict__ pos, int64_t rows,
                                                              const float* __restrict__ weight, V* __restrict__ Y) {
-  for (int64_t t = blockIdx.x; t < T; t += gridDim.x)
-    for (int64_t c = threadIdx.x; c < d; c += kThreads) {
-      float s = 0.f;
-      for (int j = 0; j < k; ++j) {
-        const int p = pos[t * k + j];
-        if (p >= 0 && p < rows) s = fmaf(weight ? weight[t * k + j] : 1.f, VT<V>::load(Ys, p * d + c), s);
+  const int64_t t = (int64_t)blockIdx.x * (kThreads / NT) + threadIdx.x / NT;
+  if (t >= T) return;
+  const int d = (int)d64;
+  for (int c = threadIdx.x % NT * kVec; c < d; c += NT * kVec) {
+    float s[kVec] = {};
+    for (int j0 = 0; j0 < k; j0 += kSlots) {
+      Vec8<V> v[kSlots];
+      float w[kSlots];
+      bool in[kSlots];
+#pragma unroll
+      for (int j = 0; j < kSlots; ++j) {
+        const int64_t slot = t * k + min(j0 + j, k - 1);
+        const int p = pos[slot];
+        in[j] = j0 + j < k && p >= 0 && p < rows;
+        w[j] = weight ? weight[slot] : 1.f;
+        if (in[j]) v[j] = load8(Ys + p * d64, c, d);
       }
-      VT<V>::store(Y, t * d + c, s);
+#pragma unroll
+      for (int j = 0; j < kSlots; ++j)
+        if (in[j])
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) s[e] = fmaf(w[j], v[j].get(e), s[e]);
     }
+    store8(Y + t * d64, c, d, s);
+  }
 }
 
-// One wave per slot.
-template <typename V>
+template <typename V, int NT>
 __global__ __launch_bounds__(kThreads) void k_expert_combine_bwd(const V* __restrict__ dY, const V* __restrict__ Ys,
-                                                                 int64_t T, int64_t d, int k,
+                                                                 int64_t T, int64_t d64, int k,
                                                                  const int32_t* __restrict__ pos, int64_t rows,
                                                                  const float* __restrict__ weight, V* __restrict__ dYs,
                                                                  float* __restrict__ dweight) {
-  const int lane = lane_id();
-  for (int64_t s = (int64_t)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave; s < T * k;
-       s += (int64_t)gridDim.x * (kThreads / kWave)) {
-    const int p = pos[s];
-    float dot = 0.f;
-    if (p >= 0 && p < rows) {
-      const float w = weight ? weight[s] : 1.f;
-      for (int64_t c = lane; c < d; c += kWave) {
-        const float g = VT<V>::load(dY, s / k * d + c);
-        if (dweight) dot = fmaf(g, VT<V>::load(Ys, p * d + c), dot);
-        if (dYs) VT<V>::store(dYs, p * d + c, w * g);
+  constexpr int W = NT > kWave ? NT / kWave : 1;
+  __shared__ float red[2][W][kSlots];
+  const int64_t t = (int64_t)blockIdx.x * (kThreads / NT) + threadIdx.x / NT;
+  if (t >= T) return;  // a whole workgroup where it has barriers
+  const int d = (int)d64;
+  int turn = 0;
+  for (int j0 = 0; j0 < k; j0 += kSlots, turn ^= 1) {
+    int p[kSlots];
+    float w[kSlots], dot[kSlots];
+#pragma unroll
+    for (int j = 0; j < kSlots; ++j) {
+      const int64_t slot = t * k + min(j0 + j, k - 1);
+      p[j] = j0 + j < k ? pos[slot] : -1;
+      if (p[j] >= rows) p[j] = -1;
+      w[j] = weight ? weight[slot] : 1.f;
+      dot[j] = 0.f;
+    }
+    for (int c = threadIdx.x % NT * kVec; c < d; c += NT * kVec) {
+      const Vec8<V> g = load8(dY + t * d64, c, d);
+      Vec8<V> v[kSlots];
+      if (dweight)
+#pragma unroll
+        for (int j = 0; j < kSlots; ++j)
+          if (p[j] >= 0) v[j] = load8(Ys + p[j] * d64, c, d);
+#pragma unroll
+      for (int j = 0; j < kSlots; ++j) {
+        if (p[j] < 0) continue;
+        if (dweight)
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) dot[j] = fmaf(g.get(e), v[j].get(e), dot[j]);
+        if (dYs) {
+          float o[kVec];
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) o[e] = w[j] * g.get(e);
+          store8(dYs + p[j] * d64, c, d, o);
+        }
       }
     }
-    dot = wave_sum(dot);
-    if (dweight && lane == 0) dweight[s] = dot;
+    if (!dweight) continue;
+#pragma unroll
+    for (int j = 0; j < kSlots; ++j) dot[j] = group_sum<(NT < kWave ? NT : kWave)>(dot[j]);
+    if (NT > kWave) {
+      if (lane_id() == 0)
+#pragma unroll
+        for (int j = 0; j < kSlots; ++j) red[turn][threadIdx.x / kWave][j] = dot[j];
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kSlots; ++j) {
+        dot[j] = 0.f;
+#pragma unroll
+        for (int x = 0; x < W; ++x) dot[j] += red[turn][x][j];
+      }
+    }
+    if (threadIdx.x % NT == 0)
+#pragma unroll
+      for (int j = 0; j < kSlots; ++j)
+        if (j0 + j < k) dweight[t * k + j0 + j] = dot[j];
   }
 }
 
-unsigned row_grid(int64_t T) { return (unsigned)std::min<int64_t>(T, 1 << 20); }
+// Calls f with the threads per token: those that one chunk each needs, up to a wave for many
+// tokens and a workgroup for few.
+template <typename F> hipError_t with_threads(int64_t T, int64_t d, F f) {
+  using std::integral_constant;
+  const int64_t n = cdiv(d, kVec);
+  if (n <= 8) return f(integral_constant<int, 8>{});
+  if (n <= 16) return f(integral_constant<int, 16>{});
+  if (n <= 32) return f(integral_constant<int, 32>{});
+  if (n <= 64 || T >= 4096) return f(integral_constant<int, 64>{});
+  return f(integral_constant<int, 256>{});
+}
+
+unsigned row_blocks(int64_t T, int nt) { return (unsigned)cdiv(T, kThreads / nt); }
 
 }  // namespace
 
-size_t expert_workspace_bytes(int64_t, int, int) { return 0; }
+size_t expert_workspace_bytes(int64_t T, int k, int E) {
+  const int64_t n = T * k;
+  return n <= kSmallSlots ? 0 : (size_t)cdiv(n, order_run(n)) * E * sizeof(int32_t);
+}
 
-hipError_t launch_expert_order(const int32_t* expert, int64_t T, int k, int E, int32_t* pos, int32_t* offsets,
-                               void*, hipStream_t s) {
-  const size_t lds = (size_t)E * (1 + kOrderThreads / kWave) * sizeof(int32_t);
+hipError_t launch_expert_dispatch(const int32_t* expert, int64_t T, int k, int E, int32_t* pos, int32_t* offsets,
+                                  const void* X, int bf16, int64_t d, int64_t rows, void* Xs, void* workspace,
+                                  hipStream_t s) {
+  const int64_t n = T * k;
+  if (n <= kSmallSlots) {
+    const dim3 grid((unsigned)T + 1);
+    if (bf16)
+      hipLaunchKernelGGL(k_expert_small<bf16_t>, grid, dim3(kThreads), 0, s, expert, (int)n, k, E, pos, offsets,
+                         (const bf16_t*)X, d, rows, (bf16_t*)Xs);
+    else
+      hipLaunchKernelGGL(k_expert_small<float>, grid, dim3(kThreads), 0, s, expert, (int)n, k, E, pos, offsets,
+                         (const float*)X, d, rows, (float*)Xs);
+    return hipGetLastError();
+  }
+  const int64_t run = order_run(n);
+  const unsigned blocks = (unsigned)cdiv(n, run);
+  const size_t lds = (size_t)E * (2 + kOrderThreads / kWave) * sizeof(int32_t);
   if (lds > (64 << 10)) {
-    const hipError_t e = hipFuncSetAttribute((const void*)k_expert_order, hipFuncAttributeMaxDynamicSharedMemorySize,
+    const hipError_t e = hipFuncSetAttribute((const void*)k_expert_place, hipFuncAttributeMaxDynamicSharedMemorySize,
                                              (int)lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(k_expert_order, dim3(1), dim3(kOrderThreads), lds, s, expert, T * k, E, pos, offsets);
-  return hipGetLastError();
-}
-
-hipError_t launch_expert_rows(const void* X, int bf16, int64_t T, int64_t d, int k, const int32_t* pos, int64_t rows,
-                              void* Xs, hipStream_t s) {
-  if (T == 0 || rows == 0) return hipSuccess;
-  if (bf16)
-    hipLaunchKernelGGL(k_expert_rows<bf16_t>, dim3(row_grid(T)), dim3(kThreads), 0, s, (const bf16_t*)X, T, d, k, pos,
-                       rows, (bf16_t*)Xs);
-  else
-    hipLaunchKernelGGL(k_expert_rows<float>, dim3(row_grid(T)), dim3(kThreads), 0, s, (const float*)X, T, d, k, pos,
-                       rows, (float*)Xs);
-  return hipGetLastError();
+  hipLaunchKernelGGL(k_expert_count, dim3(blocks), dim3(kOrderThreads), E * sizeof(int32_t), s, expert, n, run, E,
+                     (int32_t*)workspace);
+  hipLaunchKernelGGL(k_expert_place, dim3(blocks), dim3(kOrderThreads), lds, s, expert, n, run, E,
+                     (const int32_t*)workspace, pos, offsets);
+  if (!X || rows == 0) return hipGetLastError();
+  return with_threads(T, d, [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    if (bf16)
+      hipLaunchKernelGGL((k_expert_rows<bf16_t, NT>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s, (const bf16_t*)X, T,
+                         d, k, pos, rows, (bf16_t*)Xs);
+    else
+      hipLaunchKernelGGL((k_expert_rows<float, NT>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s, (const float*)X, T,
+                         d, k, pos, rows, (float*)Xs);
+    return hipGetLastError();
+  });
 }
 
 hipError_t launch_expert_combine(const void* Ys, int bf16, int64_t T, int64_t d, int k, const int32_t* pos,
                                  int64_t rows, const float* weight, void* Y, hipStream_t s) {
-  if (T == 0) return hipSuccess;
-  if (bf16)
-    hipLaunchKernelGGL(k_expert_combine<bf16_t>, dim3(row_grid(T)), dim3(kThreads), 0, s, (const bf16_t*)Ys, T, d, k,
-                       pos, rows, weight, (bf16_t*)Y);
-  else
-    hipLaunchKernelGGL(k_expert_combine<float>, dim3(row_grid(T)), dim3(kThreads), 0, s, (const float*)Ys, T, d, k,
-                       pos, rows, weight, (float*)Y);
-  return hipGetLastError();
+  return with_threads(T, d, [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    if (bf16)
+      hipLaunchKernelGGL((k_expert_combine<bf16_t, NT>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s,
+                         (const bf16_t*)Ys, T, d, k, pos, rows, weight, (bf16_t*)Y);
+    else
+      hipLaunchKernelGGL((k_expert_combine<float, NT>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s, (const float*)Ys,
+                         T, d, k, pos, rows, weight, (float*)Y);
+    return hipGetLastError();
+  });
 }
 
 hipError_t launch_expert_combine_bwd(const void* dY, const void* Ys, int bf16, int64_t T, int64_t d, int k,
                                      const int32_t* pos, int64_t rows, const float* weight, void* dYs, float* dweight,
                                      hipStream_t s) {
-  if (T == 0) return hipSuccess;
-  const unsigned grid = row_grid(cdiv(T * k, kThreads / kWave));
-  if (bf16)
-    hipLaunchKernelGGL(k_expert_combine_bwd<bf16_t>, dim3(grid), dim3(kThreads), 0, s, (const bf16_t*)dY,
-                       (const bf16_t*)Ys, T, d, k, pos, rows, weight, (bf16_t*)dYs, dweight);
-  else
-    hipLaunchKernelGGL(k_expert_combine_bwd<float>, dim3(grid), dim3(kThreads), 0, s, (const float*)dY,
-                       (const float*)Ys, T, d, k, pos, rows, weight, (float*)dYs, dweight);
-  return hipGetLastError();
+  return with_threads(T, d, [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    if (bf16)
+      hipLaunchKernelGGL((k_expert_combine_bwd<bf16_t, NT>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s,
+                         (const bf16_t*)dY, (const bf16_t*)Ys, T, d, k, pos, rows, weight, (bf16_t*)dYs, dweight);
+    else
+      hipLaunchKernelGGL((k_expert_combine_bwd<float, NT>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s,
+                         (const float*)dY, (const float*)Ys, T, d, k, pos, rows, weight, (float*)dYs, dweight);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace sfl
