@@ -52,8 +52,8 @@ __device__ __forceinline__ void count_experts(const int32_t* __restrict__ expert
   __syncthreads();
 }
 
-// Few slots: workgroup t finds the rows of token t's slots by counting over all slots, and copies
-// the token's row to them; one more workgroup writes the offsets. Every thread holds up to
+// Few slots: workgroup 1 + t finds the rows of token t's slots by counting over all slots, and
+// copies the token's row to them; workgroup 0 writes the offsets. Every thread holds up to
 // kSmallPer slots; a wave's count is a ballot per 64 slots.
 constexpr int kSmallPer = 16, kSmallSlots = kSmallPer * kThreads;
 
@@ -63,8 +63,8 @@ __global__ __launch_bounds__(kThreads) void k_expert_small(const int32_t* __rest
                                                            const V* __restrict__ X, int64_t d, int64_t rows,
                                                            V* __restrict__ Xs) {
   __shared__ int cnt[kRouteMaxExperts];  // the offsets' workgroup; [k][4] partial counts in the others
-  const int64_t t = blockIdx.x;
-  if (t == gridDim.x - 1) {
+  const int64_t t = (int64_t)blockIdx.x - 1;
+  if (t < 0) {
     count_experts(expert, 0, n, E, cnt, kThreads);
     if (threadIdx.x < kWave) {
       const int sum = scan_experts(cnt, E);
@@ -201,7 +201,11 @@ __global__ __launch_bounds__(kOrderThreads) void k_expert_place(const int32_t* _
 int64_t order_run(int64_t n) { return cdiv(cdiv(n, 256), kOrderThreads) * kOrderThreads; }
 
 // -------------------------------------------------------------------------- the rows ----
-// NT threads per token, chunk after chunk of 8 columns each; R tokens per workgroup.
+// NT threads per token, chunks of 8 columns each: as many threads as there are chunks, up to a
+// workgroup of 256 (16384 x 4096 bf16 to two of eight experts: dispatch 97 us with a wave per token,
+// 78 with 256 threads; combine 94 and 79, its gradient 167 and 141).
+
+constexpr int kRowChunks = 2;  // of a token's row, on their way together (84 -> 78 us)
 
 template <typename V, int NT>
 __global__ __launch_bounds__(kThreads) void k_expert_rows(const V* __restrict__ X, int64_t T, int64_t d64, int k,
@@ -211,18 +215,23 @@ __global__ __launch_bounds__(kThreads) void k_expert_rows(const V* __restrict__ 
   if (t >= T) return;
   const int d = (int)d64;
   const V* from = X + t * d64;
-  for (int c = threadIdx.x % NT * kVec; c < d; c += NT * kVec) {
-    const Vec8<V> v = load8(from, c, d);
+  for (int c = threadIdx.x % NT * kVec; c < d; c += kRowChunks * NT * kVec) {
+    Vec8<V> v[kRowChunks];
+#pragma unroll
+    for (int i = 0; i < kRowChunks; ++i) v[i] = load8(from, c + i * NT * kVec, d);
     for (int j = 0; j < k; ++j) {
       const int p = pos[t * k + j];
-      if (p >= 0 && p < rows) copy8(Xs + p * d64, c, d, v);
+      if (p >= 0 && p < rows)
+#pragma unroll
+        for (int i = 0; i < kRowChunks; ++i) copy8(Xs + p * d64, c + i * NT * kVec, d, v[i]);
     }
   }
 }
 
-constexpr int kSlots = 4;  // slots whose rows are in flight together
-
-template <typename V, int NT>
+// KS: slots whose rows are in flight together. Two for tokens of one or two slots (combine 79 -> 74
+// us, gradient 135 -> 127 against four), four for more (16384 x 1024 to eight of 64: 59 -> 57 and
+// 129 -> 119 us against two; eight are slower everywhere).
+template <typename V, int NT, int KS>
 __global__ __launch_bounds__(kThreads) void k_expert_combine(const V* __restrict__ Ys, int64_t T, int64_t d64, int k,
                                                              const int32_t* __restrict__ pos, int64_t rows,
                                                              const float* __restrict__ weight, V* __restrict__ Y) {
@@ -231,12 +240,12 @@ __global__ __launch_bounds__(kThreads) void k_expert_combine(const V* __restrict
   const int d = (int)d64;
   for (int c = threadIdx.x % NT * kVec; c < d; c += NT * kVec) {
     float s[kVec] = {};
-    for (int j0 = 0; j0 < k; j0 += kSlots) {
-      Vec8<V> v[kSlots];
-      float w[kSlots];
-      bool in[kSlots];
+    for (int j0 = 0; j0 < k; j0 += KS) {
+      Vec8<V> v[KS];
+      float w[KS];
+      bool in[KS];
 #pragma unroll
-      for (int j = 0; j < kSlots; ++j) {
+      for (int j = 0; j < KS; ++j) {
         const int64_t slot = t * k + min(j0 + j, k - 1);
         const int p = pos[slot];
         in[j] = j0 + j < k && p >= 0 && p < rows;
@@ -244,7 +253,7 @@ __global__ __launch_bounds__(kThreads) void k_expert_combine(const V* __restrict
         if (in[j]) v[j] = load8(Ys + p * d64, c, d);
       }
 #pragma unroll
-      for (int j = 0; j < kSlots; ++j)
+      for (int j = 0; j < KS; ++j)
         if (in[j])
 #pragma unroll
           for (int e = 0; e < kVec; ++e) s[e] = fmaf(w[j], v[j].get(e), s[e]);
@@ -253,38 +262,40 @@ __global__ __launch_bounds__(kThreads) void k_expert_combine(const V* __restrict
   }
 }
 
-template <typename V, int NT>
+template <typename V, int NT, int KS>
 __global__ __launch_bounds__(kThreads) void k_expert_combine_bwd(const V* __restrict__ dY, const V* __restrict__ Ys,
                                                                  int64_t T, int64_t d64, int k,
                                                                  const int32_t* __restrict__ pos, int64_t rows,
                                                                  const float* __restrict__ weight, V* __restrict__ dYs,
                                                                  float* __restrict__ dweight) {
   constexpr int W = NT > kWave ? NT / kWave : 1;
-  __shared__ float red[2][W][kSlots];
-  const int64_t t = (int64_t)blockIdx.x * (kThreads / NT) + threadIdx.x / NT;
-  if (t >= T) return;  // a whole workgroup where it has barriers
+  __shared__ float red[2][kThreads / NT][W][KS];
+  const int group = threadIdx.x / NT;
+  const int64_t mine = (int64_t)blockIdx.x * (kThreads / NT) + group;
+  const bool in = mine < T;  // a token past the end goes along (barriers) without slots
+  const int64_t t = in ? mine : T - 1;
   const int d = (int)d64;
   int turn = 0;
-  for (int j0 = 0; j0 < k; j0 += kSlots, turn ^= 1) {
-    int p[kSlots];
-    float w[kSlots], dot[kSlots];
+  for (int j0 = 0; j0 < k; j0 += KS, turn ^= 1) {
+    int p[KS];
+    float w[KS], dot[KS];
 #pragma unroll
-    for (int j = 0; j < kSlots; ++j) {
+    for (int j = 0; j < KS; ++j) {
       const int64_t slot = t * k + min(j0 + j, k - 1);
-      p[j] = j0 + j < k ? pos[slot] : -1;
+      p[j] = in && j0 + j < k ? pos[slot] : -1;
       if (p[j] >= rows) p[j] = -1;
       w[j] = weight ? weight[slot] : 1.f;
       dot[j] = 0.f;
     }
     for (int c = threadIdx.x % NT * kVec; c < d; c += NT * kVec) {
       const Vec8<V> g = load8(dY + t * d64, c, d);
-      Vec8<V> v[kSlots];
+      Vec8<V> v[KS];
       if (dweight)
 #pragma unroll
-        for (int j = 0; j < kSlots; ++j)
+        for (int j = 0; j < KS; ++j)
           if (p[j] >= 0) v[j] = load8(Ys + p[j] * d64, c, d);
 #pragma unroll
-      for (int j = 0; j < kSlots; ++j) {
+      for (int j = 0; j < KS; ++j) {
         if (p[j] < 0) continue;
         if (dweight)
 #pragma unroll
@@ -299,36 +310,37 @@ __global__ __launch_bounds__(kThreads) void k_expert_combine_bwd(const V* __rest
     }
     if (!dweight) continue;
 #pragma unroll
-    for (int j = 0; j < kSlots; ++j) dot[j] = group_sum<(NT < kWave ? NT : kWave)>(dot[j]);
+    for (int j = 0; j < KS; ++j) dot[j] = group_sum<(NT < kWave ? NT : kWave)>(dot[j]);
     if (NT > kWave) {
       if (lane_id() == 0)
 #pragma unroll
-        for (int j = 0; j < kSlots; ++j) red[turn][threadIdx.x / kWave][j] = dot[j];
+        for (int j = 0; j < KS; ++j) red[turn][group][threadIdx.x % NT / kWave][j] = dot[j];
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < kSlots; ++j) {
+      for (int j = 0; j < KS; ++j) {
         dot[j] = 0.f;
 #pragma unroll
-        for (int x = 0; x < W; ++x) dot[j] += red[turn][x][j];
+        for (int x = 0; x < W; ++x) dot[j] += red[turn][group][x][j];
       }
     }
-    if (threadIdx.x % NT == 0)
+    if (in && threadIdx.x % NT == 0)
 #pragma unroll
-      for (int j = 0; j < kSlots; ++j)
+      for (int j = 0; j < KS; ++j)
         if (j0 + j < k) dweight[t * k + j0 + j] = dot[j];
   }
 }
 
-// Calls f with the threads per token: those that one chunk each needs, up to a wave for many
-// tokens and a workgroup for few.
-template <typename F> hipError_t with_threads(int64_t T, int64_t d, F f) {
+// Calls f with the threads per token and the slots in flight.
+template <typename F> hipError_t with_threads(int64_t d, int k, F f) {
   using std::integral_constant;
   const int64_t n = cdiv(d, kVec);
-  if (n <= 8) return f(integral_constant<int, 8>{});
-  if (n <= 16) return f(integral_constant<int, 16>{});
-  if (n <= 32) return f(integral_constant<int, 32>{});
-  if (n <= 64 || T >= 4096) return f(integral_constant<int, 64>{});
-  return f(integral_constant<int, 256>{});
+#define SFL_NT(nt)                                                                       \
+  if (n <= nt || nt == kThreads)                                                         \
+    return k <= 2 ? f(integral_constant<int, nt>{}, integral_constant<int, 2>{})         \
+                  : f(integral_constant<int, nt>{}, integral_constant<int, 4>{});
+  SFL_NT(8) SFL_NT(16) SFL_NT(32) SFL_NT(64) SFL_NT(128) SFL_NT(256)
+#undef SFL_NT
+  return hipErrorInvalidValue;
 }
 
 unsigned row_blocks(int64_t T, int nt) { return (unsigned)cdiv(T, kThreads / nt); }
@@ -367,7 +379,7 @@ hipError_t launch_expert_dispatch(const int32_t* expert, int64_t T, int k, int E
   hipLaunchKernelGGL(k_expert_place, dim3(blocks), dim3(kOrderThreads), lds, s, expert, n, run, E,
                      (const int32_t*)workspace, pos, offsets);
   if (!X || rows == 0) return hipGetLastError();
-  return with_threads(T, d, [&](auto nt) {
+  return with_threads(d, k, [&](auto nt, auto) {
     constexpr int NT = decltype(nt)::value;
     if (bf16)
       hipLaunchKernelGGL((k_expert_rows<bf16_t, NT>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s, (const bf16_t*)X, T,
@@ -381,13 +393,13 @@ hipError_t launch_expert_dispatch(const int32_t* expert, int64_t T, int k, int E
 
 hipError_t launch_expert_combine(const void* Ys, int bf16, int64_t T, int64_t d, int k, const int32_t* pos,
                                  int64_t rows, const float* weight, void* Y, hipStream_t s) {
-  return with_threads(T, d, [&](auto nt) {
-    constexpr int NT = decltype(nt)::value;
+  return with_threads(d, k, [&](auto nt, auto ks) {
+    constexpr int NT = decltype(nt)::value, KS = decltype(ks)::value;
     if (bf16)
-      hipLaunchKernelGGL((k_expert_combine<bf16_t, NT>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s,
+      hipLaunchKernelGGL((k_expert_combine<bf16_t, NT, KS>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s,
                          (const bf16_t*)Ys, T, d, k, pos, rows, weight, (bf16_t*)Y);
     else
-      hipLaunchKernelGGL((k_expert_combine<float, NT>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s, (const float*)Ys,
+      hipLaunchKernelGGL((k_expert_combine<float, NT, KS>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s, (const float*)Ys,
                          T, d, k, pos, rows, weight, (float*)Y);
     return hipGetLastError();
   });
@@ -396,13 +408,13 @@ hipError_t launch_expert_combine(const void* Ys, int bf16, int64_t T, int64_t d,
 hipError_t launch_expert_combine_bwd(const void* dY, const void* Ys, int bf16, int64_t T, int64_t d, int k,
                                      const int32_t* pos, int64_t rows, const float* weight, void* dYs, float* dweight,
                                      hipStream_t s) {
-  return with_threads(T, d, [&](auto nt) {
-    constexpr int NT = decltype(nt)::value;
+  return with_threads(d, k, [&](auto nt, auto ks) {
+    constexpr int NT = decltype(nt)::value, KS = decltype(ks)::value;
     if (bf16)
-      hipLaunchKernelGGL((k_expert_combine_bwd<bf16_t, NT>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s,
+      hipLaunchKernelGGL((k_expert_combine_bwd<bf16_t, NT, KS>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s,
                          (const bf16_t*)dY, (const bf16_t*)Ys, T, d, k, pos, rows, weight, (bf16_t*)dYs, dweight);
     else
-      hipLaunchKernelGGL((k_expert_combine_bwd<float, NT>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s,
+      hipLaunchKernelGGL((k_expert_combine_bwd<float, NT, KS>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s,
                          (const float*)dY, (const float*)Ys, T, d, k, pos, rows, weight, (float*)dYs, dweight);
     return hipGetLastError();
   });

@@ -5,7 +5,7 @@
 // dl_i = p_i (up_i - sum_j s_j G_j), p over the chosen (normalise) or all available experts,
 // up_i = G_j for a chosen expert and 0 for another.
 #include "block.h"
-#include "common.h"
+#include "rows.h"
 
 #include <algorithm>
 
@@ -14,7 +14,6 @@ namespace sfl {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPerLane = kRouteMaxExperts / kWave;
 
 // A logit's place in the order of the reals as an unsigned number: larger logit, larger key; 0
 // for an unavailable one (-inf or NaN). -0 and +0 have one key.
@@ -27,62 +26,80 @@ __device__ __forceinline__ float key_logit(uint32_t key) {
   return __uint_as_float((key & 0x80000000u) ? (key & 0x7fffffffu) : ~key);
 }
 
-__device__ __forceinline__ uint64_t wave_max64(uint64_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const uint64_t u = __shfl_xor((unsigned long long)v, o, 64);
-    v = u > v ? u : v;
-  }
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false));
+}
+
+// Largest value of aligned groups of G lanes, in every lane (lanes trade as in group_sum).
+template <int G> __device__ __forceinline__ uint32_t group_max(uint32_t v) {
+  v = dpp_max<0xB1>(v);
+  v = dpp_max<0x4E>(v);
+  v = dpp_max<0x141>(v);
+  if (G >= 16) v = dpp_max<0x140>(v);
+  if (G == 32) v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
+  if (G == 64)
+    v = max(max((uint32_t)readlane_i((int)v, 0), (uint32_t)readlane_i((int)v, 16)),
+            max((uint32_t)readlane_i((int)v, 32), (uint32_t)readlane_i((int)v, 48)));
   return v;
 }
 
-// One wave per token; lane l holds experts l, l + 64, ...
-template <typename V>
+// G lanes per token, lane x with the PL experts x PL .. x PL + PL - 1 (so the lowest lane with the
+// largest key has the lowest index). k rounds: the group's largest key, the first lane that has it,
+// and that lane drops its first expert with it. Lane j keeps the j-th choice. What bounds it is the
+// chain of the k rounds: about 12 instructions each for 64 experts, nothing through LDS
+// (16384 tokens, 8 of 64: 45 us with 64-bit shuffles over LDS, one wave per token).
+template <typename V, int G, int PL>
 __global__ __launch_bounds__(kThreads) void k_route_fwd(const V* __restrict__ logits, int64_t T, int E, int k,
                                                         int normalise, float scale, int32_t* __restrict__ expert,
                                                         float* __restrict__ weight) {
-  const int lane = lane_id();
-  const int64_t t = (int64_t)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
-  if (t >= T) return;
-  uint32_t key[kPerLane];
+  const int lane = lane_id(), x = lane % G;
+  const int64_t mine_t = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
+  const int64_t t = min(mine_t, T - 1);  // groups past the end repeat the last token and store nothing
+  uint32_t key[PL], best = 0u;
 #pragma unroll
-  for (int i = 0; i < kPerLane; ++i) {
-    const int e = lane + kWave * i;
+  for (int i = 0; i < PL; ++i) {
+    const int e = x * PL + i;
     key[i] = e < E ? order_key(VT<V>::load(logits, t * E + e)) : 0u;
+    best = max(best, key[i]);
   }
-  float top = 0.f, all = 0.f, chosen = 0.f, mine = 0.f;
+  float all = 0.f, top = 0.f;
+  uint32_t my_key = 0u;
   int my_expert = -1;
   for (int j = 0; j < k; ++j) {
-    uint64_t best = 0;  // key, then the lower index
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i) {
-      const uint64_t c = ((uint64_t)key[i] << 32) | (uint32_t)~(lane + kWave * i);
-      best = key[i] && c > best ? c : best;
-    }
-    best = wave_max64(best);
-    if (best == 0) break;
-    const int e = (int)~(uint32_t)best;
-    const float l = key_logit((uint32_t)(best >> 32));
+    const uint32_t m = group_max<G>(best);
     if (j == 0) {
-      top = l;
+      top = key_logit(m);  // not used where m is 0
+      if (!normalise) {
 #pragma unroll
-      for (int i = 0; i < kPerLane; ++i)
-        if (key[i]) all += expf(key_logit(key[i]) - top);
-      all = wave_sum(all);
+        for (int i = 0; i < PL; ++i) all += key[i] ? expf(key_logit(key[i]) - top) : 0.f;
+        all = group_sum<G>(all);
+      }
     }
-    const float v = expf(l - top);
-    chosen += v;
-    if (lane == j) {
-      mine = v;
-      my_expert = e;
-    }
+    const uint64_t have = ballot(best == m) >> (lane - x);  // m of this lane's group
+    const int first = __builtin_ctzll(have);
+    int at = -1;
+    if (x == first && m) {
+      best = 0u;
 #pragma unroll
-    for (int i = 0; i < kPerLane; ++i)
-      if (lane + kWave * i == e) key[i] = 0u;
+      for (int i = 0; i < PL; ++i) {
+        if (at < 0 && key[i] == m) {
+          at = i;
+          key[i] = 0u;
+        }
+        best = max(best, key[i]);
+      }
+    }
+    if (PL > 1) at = __shfl(at, (lane - x) + first, 64);
+    if (x == j && m) {
+      my_key = m;
+      my_expert = PL > 1 ? first * PL + at : first;
+    }
   }
-  if (lane < k) {
-    expert[t * k + lane] = my_expert;
-    weight[t * k + lane] = my_expert < 0 ? 0.f : scale * (mine / (normalise ? chosen : all));
+  const float mine = my_expert >= 0 ? expf(key_logit(my_key) - top) : 0.f;
+  const float Z = normalise ? group_sum<G>(mine) : all;
+  if (x < k && mine_t < T) {
+    expert[t * k + x] = my_expert;
+    weight[t * k + x] = my_expert >= 0 ? scale * (mine / Z) : 0.f;
   }
 }
 
@@ -138,16 +155,30 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const V* __restrict__ lo
 
 }  // namespace
 
+template <typename V, int G, int PL>
+hipError_t route_fwd(const void* logits, int64_t T, int E, int k, int normalise, float scale, int32_t* expert,
+                     float* weight, hipStream_t s) {
+  hipLaunchKernelGGL((k_route_fwd<V, G, PL>), dim3((unsigned)cdiv(T, kThreads / G)), dim3(kThreads), 0, s,
+                     (const V*)logits, T, E, k, normalise, scale, expert, weight);
+  return hipGetLastError();
+}
+
 hipError_t launch_route_fwd(const void* logits, int bf16, int64_t T, int E, int k, int normalise, float scale,
                             int32_t* expert, float* weight, hipStream_t s) {
-  const dim3 grid((unsigned)cdiv(T, kThreads / kWave));
-  if (bf16)
-    hipLaunchKernelGGL(k_route_fwd<bf16_t>, grid, dim3(kThreads), 0, s, (const bf16_t*)logits, T, E, k, normalise,
-                       scale, expert, weight);
-  else
-    hipLaunchKernelGGL(k_route_fwd<float>, grid, dim3(kThreads), 0, s, (const float*)logits, T, E, k, normalise, scale,
-                       expert, weight);
-  return hipGetLastError();
+#define SFL_ROUTE(e, g, pl)                                                                                \
+  if (E <= e)                                                                                              \
+    return bf16 ? route_fwd<bf16_t, g, pl>(logits, T, E, k, normalise, scale, expert, weight, s)           \
+                : route_fwd<float, g, pl>(logits, T, E, k, normalise, scale, expert, weight, s);
+  SFL_ROUTE(8, 8, 1)
+  SFL_ROUTE(16, 16, 1)
+  SFL_ROUTE(32, 32, 1)
+  SFL_ROUTE(64, 64, 1)
+  SFL_ROUTE(128, 64, 2)
+  SFL_ROUTE(256, 64, 4)
+  SFL_ROUTE(512, 64, 8)
+  SFL_ROUTE(kRouteMaxExperts, 64, 16)
+#undef SFL_ROUTE
+  return hipErrorInvalidValue;
 }
 
 hipError_t launch_route_bwd(const void* logits, int bf16, int64_t T, int E, int k, int normalise, float scale,
