@@ -159,8 +159,14 @@ def _ptr(t):
     return t.data_ptr()
 
 
+# torch's handle of the current stream without the Stream object around it (2.9 against 0.3 us a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 

@@ -1,9 +1,14 @@
 // Global norm of a list of gradients and clipping: q = sum g^2 over all tensors, norm = sqrt(q),
 // g <- c g with c = max_norm / norm where norm > max_norm, else 1 (a norm that is not finite
 // scales nothing). Squares are formed and added in 64 bits, so no finite gradient overflows or
-// underflows the sum, and the order of the sums is fixed: blocks of a launch, then launches.
+// underflows the sum (the conversions and fp64 FMAs stay far below the rate the values arrive at),
+// and the order of the sums is fixed: a thread's, a workgroup's, then the workgroups'.
+//
+// Bound by memory: the list is read twice and written once. The second pass walks the list from
+// its end, where the first one stopped: the last 256 MiB that were read are still in the infinity
+// cache, and the scaled values are stored non-temporally beside them.
 #include "block.h"
-#include "common.h"
+#include "rows.h"
 
 #include <algorithm>
 
@@ -12,16 +17,28 @@ namespace sfl {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kListMax = 112;        // tensors of one launch: the list travels as a kernel argument
-constexpr int64_t kChunk = 1 << 14;  // elements of one block
+constexpr int kListMax = 112;    // tensors of one launch: the list travels as a kernel argument
+constexpr int kTile = kThreads * kVec;  // elements of one step of a workgroup
+
+// Elements of a workgroup's share: all of its loads go out together. Long shares are slower (their
+// last round leaves CUs idle; both passes over 2^27 fp32 elements in two tensors: 304 us with shares
+// of 65536, 303 with 8192, 290 with 8192 and 4096; over 192 tensors 339 and 303), shorter ones too
+// (2048: 308 us). Short lists take smaller shares so that more CUs work.
+constexpr int kSumShare = 4 * kTile, kScaleShare = 2 * kTile;
+int64_t share_of(int64_t total, int64_t most) {
+  int64_t share = kTile;
+  while (share < most && total / share > 1024) share *= 2;
+  return share;
+}
 
 struct GradList {
   const void* src[kListMax];
   void* dst[kListMax];
   int64_t n[kListMax];
-  int32_t first[kListMax + 1];  // first block of each tensor
+  int32_t first[kListMax + 1];  // first workgroup of each tensor
   uint8_t bf16[kListMax];
   int32_t count;
+  int32_t share;
 };
 
 __device__ __forceinline__ int tensor_of(const GradList& l, int block) {
@@ -36,115 +53,163 @@ __device__ __forceinline__ int tensor_of(const GradList& l, int block) {
   return lo;
 }
 
-__device__ __forceinline__ double block_sum(double v) {
-  __shared__ double red[kThreads / kWave];
+// Sum over N threads in the first of them, in a fixed order.
+template <int N> __device__ __forceinline__ double block_sum(double v) {
+  __shared__ double red[N / kWave];
   v = wave_sum(v);
   if (lane_id() == 0) red[threadIdx.x / kWave] = v;
   __syncthreads();
   double s = red[0];
-  for (int w = 1; w < kThreads / kWave; ++w) s += red[w];
+  for (int w = 1; w < N / kWave; ++w) s += red[w];
   return s;
 }
 
-template <typename V>
-__device__ __forceinline__ double chunk_sumsq(const V* p, int64_t i0, int64_t i1) {
-  double s = 0;
-  for (int64_t i = i0 + threadIdx.x; i < i1; i += kThreads) {
-    const double g = (double)VT<V>::load(p, i);
-    s = fma(g, g, s);
-  }
-  return s;
+template <typename V> __device__ __forceinline__ double share_sumsq(const V* p, int n) {
+  double s[2] = {0, 0};
+  constexpr int kSteps = kSumShare / kTile;
+  const int c = threadIdx.x * kVec;
+  Vec8<V> v[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) v[i] = load8(p, c + i * kTile, n);
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      const double g = (double)v[i].get(e);
+      s[e & 1] = fma(g, g, s[e & 1]);
+    }
+  return s[0] + s[1];
 }
 
 __global__ __launch_bounds__(kThreads) void k_grad_sumsq(GradList l, double* __restrict__ part) {
   const int b = blockIdx.x, i = tensor_of(l, b);
-  const int64_t i0 = (int64_t)(b - l.first[i]) * kChunk, i1 = min(i0 + kChunk, l.n[i]);
-  const double s = block_sum(l.bf16[i] ? chunk_sumsq((const bf16_t*)l.src[i], i0, i1)
-                                       : chunk_sumsq((const float*)l.src[i], i0, i1));
+  const int64_t at = (int64_t)(b - l.first[i]) * l.share;
+  const int n = (int)min((int64_t)l.share, l.n[i] - at);
+  const double s = block_sum<kThreads>(l.bf16[i] ? share_sumsq((const bf16_t*)l.src[i] + at, n)
+                                                 : share_sumsq((const float*)l.src[i] + at, n));
   if (threadIdx.x == 0) part[b] = s;
 }
 
-__global__ __launch_bounds__(kThreads) void k_grad_sum(const double* __restrict__ part, int64_t n,
-                                                       double* __restrict__ sumsq) {
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void k_grad_sum(const double* __restrict__ part, int64_t n,
+                                                          double* __restrict__ sumsq) {
   double s = 0;
-  for (int64_t i = threadIdx.x; i < n; i += kThreads) s += part[i];
-  s = block_sum(s);
+  for (int64_t i0 = threadIdx.x; i0 < n; i0 += 4 * kSumThreads) {
+    double q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = part[min(i0 + i * kSumThreads, n - 1)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s += i0 + i * kSumThreads < n ? q[i] : 0.0;
+  }
+  s = block_sum<kSumThreads>(s);
   if (threadIdx.x == 0) *sumsq = s;
 }
 
-template <typename V>
-__device__ __forceinline__ void chunk_scale(const V* p, V* q, int64_t i0, int64_t i1, float c) {
-  if (p == q && c == 1.f) return;
-  for (int64_t i = i0 + threadIdx.x; i < i1; i += kThreads) VT<V>::store(q, i, VT<V>::load(p, i) * c);
+template <typename V> __device__ __forceinline__ void share_scale(const V* p, V* q, int n, float by) {
+  if (p == q && by == 1.f) return;
+  constexpr int kSteps = kScaleShare / kTile;
+  const int c = threadIdx.x * kVec;
+  Vec8<V> v[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) v[i] = load8(p, c + i * kTile, n);
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    float o[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) o[e] = v[i].get(e) * by;
+    store8(q, c + i * kTile, n, o);
+  }
 }
 
 __global__ __launch_bounds__(kThreads) void k_grad_scale(GradList l, const double* __restrict__ sumsq, float max_norm,
                                                          float* __restrict__ norm) {
   const double nrm = sqrt(*sumsq);
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)nrm;
-  const float c = nrm > (double)max_norm && nrm < (double)INFINITY ? (float)((double)max_norm / nrm) : 1.f;
+  const float by = nrm > (double)max_norm && nrm < (double)INFINITY ? (float)((double)max_norm / nrm) : 1.f;
   if (l.count == 0) return;
-  const int b = blockIdx.x, i = tensor_of(l, b);
-  const int64_t i0 = (int64_t)(b - l.first[i]) * kChunk, i1 = min(i0 + kChunk, l.n[i]);
+  const int b = gridDim.x - 1 - blockIdx.x, i = tensor_of(l, b);
+  const int64_t at = (int64_t)(b - l.first[i]) * l.share;
+  const int n = (int)min((int64_t)l.share, l.n[i] - at);
   if (l.bf16[i])
-    chunk_scale((const bf16_t*)l.src[i], (bf16_t*)l.dst[i], i0, i1, c);
+    share_scale((const bf16_t*)l.src[i] + at, (bf16_t*)l.dst[i] + at, n, by);
   else
-    chunk_scale((const float*)l.src[i], (float*)l.dst[i], i0, i1, c);
+    share_scale((const float*)l.src[i] + at, (float*)l.dst[i] + at, n, by);
 }
 
-int64_t chunks_of(int64_t n) { return cdiv(n, kChunk); }
+int64_t elements(const sfl_grad_t* list, int n) {
+  int64_t total = 0;
+  for (int i = 0; i < n; ++i) total += list[i].n;
+  return total;
+}
 
-// Calls f(list, blocks) for each launch's share of the tensors.
-template <typename F>
-void each_launch(const sfl_grad_t* list, int n, F f) {
-  GradList l;
-  l.count = 0;
+// Fills l with tensors from list[i] on (from its end where `back`) and moves i past them; returns
+// the launch's workgroups, 0 at the end of the list.
+int64_t next_launch(const sfl_grad_t* list, int n, bool back, int64_t share, int* i, GradList* l) {
+  int begin = *i, end = *i, held = 0;
   int64_t blocks = 0;
-  for (int i = 0; i < n; ++i) {
-    const int64_t c = chunks_of(list[i].n);
-    if (c == 0) continue;
-    if (l.count == kListMax || blocks + c > INT32_MAX) {
-      f(l, blocks);
-      l.count = 0;
-      blocks = 0;
-    }
-    l.src[l.count] = list[i].src;
-    l.dst[l.count] = list[i].dst ? list[i].dst : const_cast<void*>(list[i].src);
-    l.n[l.count] = list[i].n;
-    l.bf16[l.count] = list[i].dtype == SFL_BF16;
-    l.first[l.count++] = (int32_t)blocks;
+  for (; *i < n; ++*i) {
+    const int64_t c = cdiv(list[back ? n - 1 - *i : *i].n, share);
+    if (held + (c > 0) > kListMax || blocks + c > INT32_MAX) break;
+    held += c > 0;
     blocks += c;
-    l.first[l.count] = (int32_t)blocks;
+    end = *i + 1;
   }
-  if (blocks) f(l, blocks);
+  if (back) {
+    const int b = n - end;
+    end = n - begin;
+    begin = b;
+  }
+  l->count = 0;
+  l->share = (int32_t)share;
+  l->first[0] = 0;
+  for (int j = begin; j < end; ++j) {
+    const int64_t c = cdiv(list[j].n, share);
+    if (c == 0) continue;
+    const int m = l->count++;
+    l->src[m] = list[j].src;
+    l->dst[m] = list[j].dst ? list[j].dst : const_cast<void*>(list[j].src);
+    l->n[m] = list[j].n;
+    l->bf16[m] = list[j].dtype == SFL_BF16;
+    l->first[m + 1] = l->first[m] + (int32_t)c;
+  }
+  return blocks;
 }
 
 }  // namespace
 
 size_t grad_workspace_bytes(const sfl_grad_t* list, int n) {
+  const int64_t share = share_of(elements(list, n), kSumShare);
   int64_t blocks = 0;
-  for (int i = 0; i < n; ++i) blocks += chunks_of(list[i].n);
+  for (int i = 0; i < n; ++i) blocks += cdiv(list[i].n, share);
   return (size_t)blocks * sizeof(double);
 }
 
 hipError_t launch_grad_sumsq(const sfl_grad_t* list, int n, double* sumsq, double* part, hipStream_t s) {
-  int64_t total = 0;
-  each_launch(list, n, [&](const GradList& l, int64_t blocks) {
-    hipLaunchKernelGGL(k_grad_sumsq, dim3((unsigned)blocks), dim3(kThreads), 0, s, l, part + total);
-    total += blocks;
-  });
-  hipLaunchKernelGGL(k_grad_sum, dim3(1), dim3(kThreads), 0, s, part, total, sumsq);
+  const int64_t share = share_of(elements(list, n), kSumShare);
+  int64_t done = 0;
+  GradList l;
+  for (int i = 0; i < n;) {
+    const int64_t blocks = next_launch(list, n, false, share, &i, &l);
+    if (blocks)
+      hipLaunchKernelGGL(k_grad_sumsq, dim3((unsigned)blocks), dim3(kThreads), 0, s, l, part + done);
+    done += blocks;
+  }
+  hipLaunchKernelGGL(k_grad_sum, dim3(1), dim3(kSumThreads), 0, s, part, done, sumsq);
   return hipGetLastError();
 }
 
 hipError_t launch_grad_clip(const sfl_grad_t* list, int n, const double* sumsq, float max_norm, float* norm,
                             hipStream_t s) {
-  each_launch(list, n, [&](const GradList& l, int64_t blocks) {
+  const int64_t share = share_of(elements(list, n), kScaleShare);
+  GradList l;
+  l.count = 0;
+  for (int i = 0; i < n;) {
+    const int64_t blocks = next_launch(list, n, true, share, &i, &l);
+    if (!blocks) continue;
     hipLaunchKernelGGL(k_grad_scale, dim3((unsigned)blocks), dim3(kThreads), 0, s, l, sumsq, max_norm, norm);
     norm = nullptr;  // the first launch writes it
-  });
+  }
   if (norm) {
-    GradList l;
     l.count = 0;
     hipLaunchKernelGGL(k_grad_scale, dim3(1), dim3(kThreads), 0, s, l, sumsq, max_norm, norm);
   }
