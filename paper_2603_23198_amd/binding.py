@@ -10,7 +10,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-from array import array
 from ctypes import POINTER, Structure, c_char_p, c_double, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
@@ -22,6 +21,8 @@ if not os.path.exists(LIB_PATH):
     raise ImportError(f"libsfl.so not found at {LIB_PATH}; build it with "
                       "`python -m paper_2603_23198_amd.build` (or __graft_entry__.build())")
 _lib = ctypes.CDLL(LIB_PATH)
+
+from . import _marshal  # noqa: E402  (built beside libsfl.so)
 
 SFL_F32, SFL_BF16 = 0, 1
 SFL_OK, SFL_E_ARG, SFL_E_UNSUPPORTED, SFL_E_WORKSPACE, SFL_E_HIP = 0, -1, -2, -3, -4
@@ -171,7 +172,13 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+_CODES = {torch.float32: SFL_F32, torch.bfloat16: SFL_BF16, "f32": SFL_F32, "bf16": SFL_BF16}
+
+
 def dtype_code(dtype):
+    code = _CODES.get(dtype)
+    if code is not None:
+        return code
     if dtype in ("bf16", torch.bfloat16, SFL_BF16):
         return SFL_BF16
     if dtype in ("f32", torch.float32, SFL_F32):
@@ -375,17 +382,10 @@ def sfl_transpose(inp, out, stream=None):
 
 # ---- around the layer: norms, router, experts, gradient clipping ----
 # These take the tensors themselves, so shapes, types and contiguity are checked here.
-_F32, _I32 = torch.float32, torch.int32
-
-
-def _buf(t, dtype, n):
-    """Device pointer of a contiguous tensor of n elements of dtype; None stays None."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"expected a contiguous {dtype} tensor of {n} elements, got {t.dtype} {tuple(t.shape)}"
-                         f"{'' if t.is_contiguous() else ' (not contiguous)'}")
-    return t.data_ptr()
+# Device pointer of a contiguous device tensor of n elements of a type (SFL_F32, SFL_BF16 or one of
+# the two below), None for None; ValueError for any other.
+_buf = _marshal.ptr
+_F32, _I32, _F64 = SFL_F32, 2, 3
 
 
 def _space(workspace):
@@ -395,8 +395,8 @@ def _space(workspace):
 def sfl_norm_forward(X, Y=None, *, X_out=None, N=None, norms=SFL_NORM_PRE | SFL_NORM_POST, w_pre=None, w_post=None,
                      gate_c=None, gate_t=None, res_scale=1.0, eps=1e-6, stream=None):
     T, d = X.shape
-    dt, n = X.dtype, T * d
-    a = NormArgs(dtype_code(dt), norms, T, d, eps, res_scale, _buf(X, dt, n), _buf(Y, dt, n), _buf(w_pre, _F32, d),
+    dt, n = dtype_code(X.dtype), T * d
+    a = NormArgs(dt, norms, T, d, eps, res_scale, _buf(X, dt, n), _buf(Y, dt, n), _buf(w_pre, _F32, d),
                  _buf(w_post, _F32, d), _buf(gate_c, _F32, d), _buf(gate_t, _F32, T), _buf(X_out, dt, n),
                  _buf(N, dt, n))
     _check("sfl_norm_forward", _lib.sfl_norm_forward(a, _stream(stream)))
@@ -413,8 +413,8 @@ def sfl_norm_backward(X_out, Y, dX_out, dN=None, *, dX=None, dY=None, dw_pre=Non
                       gate_t=None, res_scale=1.0, eps=1e-6, workspace=None, stream=None):
     like = X_out if X_out is not None else dX_out
     T, d = like.shape
-    dt, n = like.dtype, T * d
-    a = NormBwdArgs(dtype_code(dt), norms, T, d, eps, res_scale, _buf(X_out, dt, n), _buf(Y, dt, n),
+    dt, n = dtype_code(like.dtype), T * d
+    a = NormBwdArgs(dt, norms, T, d, eps, res_scale, _buf(X_out, dt, n), _buf(Y, dt, n),
                     _buf(w_pre, _F32, d), _buf(w_post, _F32, d), _buf(gate_c, _F32, d), _buf(gate_t, _F32, T),
                     _buf(dX_out, dt, n), _buf(dN, dt, n), _buf(dX, dt, n), _buf(dY, dt, n), _buf(dw_pre, _F32, d),
                     _buf(dw_post, _F32, d), _buf(dgate_c, _F32, d), _buf(dgate_t, _F32, T), *_space(workspace))
@@ -422,16 +422,16 @@ def sfl_norm_backward(X_out, Y, dX_out, dN=None, *, dX=None, dY=None, dw_pre=Non
 
 
 def sfl_route_forward(logits, expert, weight, *, normalise=True, scale=1.0, stream=None):
-    (T, E), k, dt = logits.shape, expert.shape[1], logits.dtype
+    (T, E), k, dt = logits.shape, expert.shape[1], dtype_code(logits.dtype)
     _check("sfl_route_forward",
-           _lib.sfl_route_forward(_buf(logits, dt, T * E), dtype_code(dt), T, E, k, 1 if normalise else 0, scale,
+           _lib.sfl_route_forward(_buf(logits, dt, T * E), dt, T, E, k, 1 if normalise else 0, scale,
                                   _buf(expert, _I32, T * k), _buf(weight, _F32, T * k), _stream(stream)))
 
 
 def sfl_route_backward(logits, expert, dweight, dlogits, *, normalise=True, scale=1.0, stream=None):
-    (T, E), k, dt = logits.shape, expert.shape[1], logits.dtype
+    (T, E), k, dt = logits.shape, expert.shape[1], dtype_code(logits.dtype)
     _check("sfl_route_backward",
-           _lib.sfl_route_backward(_buf(logits, dt, T * E), dtype_code(dt), T, E, k, 1 if normalise else 0, scale,
+           _lib.sfl_route_backward(_buf(logits, dt, T * E), dt, T, E, k, 1 if normalise else 0, scale,
                                    _buf(expert, _I32, T * k), _buf(dweight, _F32, T * k), _buf(dlogits, dt, T * E),
                                    _stream(stream)))
 
@@ -447,7 +447,7 @@ def sfl_expert_dispatch(expert, E, pos, offsets, *, X=None, Xs=None, workspace=N
     n, dt, d, rows, px, ps = T * k, SFL_F32, 1, 0, None, None
     if X is not None:
         d, rows, dt = X.shape[1], Xs.shape[0], dtype_code(X.dtype)
-        px, ps = _buf(X, X.dtype, T * d), _buf(Xs, X.dtype, rows * d)
+        px, ps = _buf(X, dt, T * d), _buf(Xs, dt, rows * d)
     ws, ws_bytes = _space(workspace)
     _check("sfl_expert_dispatch",
            _lib.sfl_expert_dispatch(_buf(expert, _I32, n), T, k, E, _buf(pos, _I32, n), _buf(offsets, _I32, E + 1), px,
@@ -455,17 +455,17 @@ def sfl_expert_dispatch(expert, E, pos, offsets, *, X=None, Xs=None, workspace=N
 
 
 def sfl_expert_combine(Ys, pos, Y, *, weight=None, stream=None):
-    (T, k), (rows, d), dt = pos.shape, Ys.shape, Ys.dtype
+    (T, k), (rows, d), dt = pos.shape, Ys.shape, dtype_code(Ys.dtype)
     _check("sfl_expert_combine",
-           _lib.sfl_expert_combine(_buf(Ys, dt, rows * d), dtype_code(dt), T, d, k, _buf(pos, _I32, T * k), rows,
+           _lib.sfl_expert_combine(_buf(Ys, dt, rows * d), dt, T, d, k, _buf(pos, _I32, T * k), rows,
                                    _buf(weight, _F32, T * k), _buf(Y, dt, T * d), _stream(stream)))
 
 
 def sfl_expert_combine_backward(dY, Ys, pos, weight, *, dYs=None, dweight=None, stream=None):
-    (T, k), d, dt = pos.shape, dY.shape[1], dY.dtype
+    (T, k), d, dt = pos.shape, dY.shape[1], dtype_code(dY.dtype)
     rows = (dYs if Ys is None else Ys).shape[0]
     _check("sfl_expert_combine_backward",
-           _lib.sfl_expert_combine_backward(_buf(dY, dt, T * d), _buf(Ys, dt, rows * d), dtype_code(dt), T, d, k,
+           _lib.sfl_expert_combine_backward(_buf(dY, dt, T * d), _buf(Ys, dt, rows * d), dt, T, d, k,
                                             _buf(pos, _I32, T * k), rows, _buf(weight, _F32, T * k),
                                             _buf(dYs, dt, rows * d), _buf(dweight, _F32, T * k), _stream(stream)))
 
@@ -473,10 +473,7 @@ def sfl_expert_combine_backward(dY, Ys, pos, weight, *, dYs=None, dweight=None, 
 def grad_list(grads, out=None):
     """The list of gradients that the sfl_grad_* calls take; it keeps the tensors alive. out: where
     the clipped gradients go, in place if None."""
-    rows = array("q")  # Grad's fields, 8 bytes each (dtype and reserved together)
-    for i, g in enumerate(grads):
-        dt, n = g.dtype, g.numel()
-        rows.extend((_buf(g, dt, n) or 0, 0 if out is None else _buf(out[i], dt, n) or 0, n, dtype_code(dt)))
+    rows = _marshal.grads(grads, out)
     a = (Grad * len(grads)).from_buffer(rows) if rows else (Grad * 0)()
     a._keepalive = (grads, out)
     return a
@@ -489,12 +486,12 @@ def sfl_grad_workspace_size(grads):
 
 
 def sfl_grad_sumsq(grads, sumsq, *, workspace=None, stream=None):
-    _check("sfl_grad_sumsq", _lib.sfl_grad_sumsq(grads, len(grads), _buf(sumsq, torch.float64, 1), *_space(workspace),
+    _check("sfl_grad_sumsq", _lib.sfl_grad_sumsq(grads, len(grads), _buf(sumsq, _F64, 1), *_space(workspace),
                                                  _stream(stream)))
 
 
 def sfl_grad_clip(grads, sumsq, max_norm, norm=None, *, stream=None):
-    _check("sfl_grad_clip", _lib.sfl_grad_clip(grads, len(grads), _buf(sumsq, torch.float64, 1), max_norm,
+    _check("sfl_grad_clip", _lib.sfl_grad_clip(grads, len(grads), _buf(sumsq, _F64, 1), max_norm,
                                                _buf(norm, _F32, 1), _stream(stream)))
 
 

@@ -1,4 +1,5 @@
-"""Build libsfl.so (HIP kernels for gfx950 + the C ABI) in-tree with hipcc.
+"""Build libsfl.so (HIP kernels for gfx950 + the C ABI) in-tree with hipcc, and the
+binding's `_marshal.so` (tensors to checked pointers) with the host compiler.
 
 Every source under csrc/ is compiled to an object file in parallel, then linked
 into `libsfl.so` next to this file. The build always recompiles (it is the
@@ -12,11 +13,13 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsfl.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 ARCH = "gfx950"  # the kernels use CDNA4 instructions (MFMA 16x16x32 bf16, ds_read_b64_tr_b16)
 
 FLAGS = [
@@ -47,6 +50,23 @@ def _compile(src, obj, extra=()):
     return errs
 
 
+def build_marshal() -> str:
+    """Compile the binding's extension module against the installed torch (host code only)."""
+    import torch
+    at = os.path.dirname(torch.__file__)
+    cxx = shutil.which("g++") or shutil.which("c++") or hipcc()
+    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+           "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(at, "include"),
+           "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+           os.path.join(CSRC, "python", "marshal.cpp"), "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu",
+           "-lc10", "-Wl,-rpath," + os.path.join(at, "lib"), "-o", MARSHAL + ".tmp"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compiling marshal.cpp failed:\n{r.stderr}")
+    os.replace(MARSHAL + ".tmp", MARSHAL)
+    return MARSHAL
+
+
 def build(verbose=False, jobs=None, extra_flags=(), out=None, csrc=None) -> str:
     """Compile and link; `extra_flags` go to every hipcc line, `out` overrides the library
     path and `csrc` the source directory."""
@@ -54,7 +74,8 @@ def build(verbose=False, jobs=None, extra_flags=(), out=None, csrc=None) -> str:
     src_dir = csrc or CSRC
     srcs = sorted(glob.glob(os.path.join(src_dir, "*.hip")) + glob.glob(os.path.join(src_dir, "*.cpp")))
     jobs = jobs or min(len(srcs), max(1, (os.cpu_count() or 4)), 16)
-    with tempfile.TemporaryDirectory(prefix="sfl_build_") as tmp:
+    with tempfile.TemporaryDirectory(prefix="sfl_build_") as tmp, cf.ThreadPoolExecutor(1) as side:
+        marshal = side.submit(build_marshal)
         objs = [os.path.join(tmp, os.path.basename(s) + ".o") for s in srcs]
         with cf.ThreadPoolExecutor(jobs) as ex:
             for src, msg in zip(srcs, ex.map(lambda a, o: _compile(a, o, extra_flags), srcs, objs)):
@@ -66,6 +87,7 @@ def build(verbose=False, jobs=None, extra_flags=(), out=None, csrc=None) -> str:
         if r.returncode != 0:
             raise RuntimeError(f"link failed:\n{r.stderr}")
         os.replace(tmp_lib, lib)
+        marshal.result()
     return lib
 
 

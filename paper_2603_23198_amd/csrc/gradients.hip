@@ -17,7 +17,7 @@ namespace sfl {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kListMax = 112;    // tensors of one launch: the list travels as a kernel argument
+constexpr int kListMax = 112;  // ranges of one launch: the list travels as a kernel argument
 constexpr int kTile = kThreads * kVec;  // elements of one step of a workgroup
 
 // Elements of a workgroup's share: all of its loads go out together. Long shares are slower (their
@@ -35,13 +35,13 @@ struct GradList {
   const void* src[kListMax];
   void* dst[kListMax];
   int64_t n[kListMax];
-  int32_t first[kListMax + 1];  // first workgroup of each tensor
+  int32_t first[kListMax + 1];  // first workgroup of each range
   uint8_t bf16[kListMax];
   int32_t count;
   int32_t share;
 };
 
-__device__ __forceinline__ int tensor_of(const GradList& l, int block) {
+__device__ __forceinline__ int range_of(const GradList& l, int block) {
   int lo = 0, hi = l.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
@@ -82,7 +82,7 @@ template <typename V> __device__ __forceinline__ double share_sumsq(const V* p, 
 }
 
 __global__ __launch_bounds__(kThreads) void k_grad_sumsq(GradList l, double* __restrict__ part) {
-  const int b = blockIdx.x, i = tensor_of(l, b);
+  const int b = blockIdx.x, i = range_of(l, b);
   const int64_t at = (int64_t)(b - l.first[i]) * l.share;
   const int n = (int)min((int64_t)l.share, l.n[i] - at);
   const double s = block_sum<kThreads>(l.bf16[i] ? share_sumsq((const bf16_t*)l.src[i] + at, n)
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_scale(GradList l, const doubl
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)nrm;
   const float by = nrm > (double)max_norm && nrm < (double)INFINITY ? (float)((double)max_norm / nrm) : 1.f;
   if (l.count == 0) return;
-  const int b = gridDim.x - 1 - blockIdx.x, i = tensor_of(l, b);
+  const int b = gridDim.x - 1 - blockIdx.x, i = range_of(l, b);
   const int64_t at = (int64_t)(b - l.first[i]) * l.share;
   const int n = (int)min((int64_t)l.share, l.n[i] - at);
   if (l.bf16[i])
@@ -142,16 +142,32 @@ int64_t elements(const sfl_grad_t* list, int n) {
   return total;
 }
 
-// Fills l with tensors from list[i] on (from its end where `back`) and moves i past them; returns
-// the launch's workgroups, 0 at the end of the list.
+const char* target(const sfl_grad_t& g) { return (const char*)(g.dst ? g.dst : g.src); }
+
+// Whether b's elements lie right behind a's, at the source and at the target (views of one bucket
+// mostly do): the two then go as one range, with fewer launches and no ragged shares.
+bool follows(const sfl_grad_t& a, const sfl_grad_t& b) {
+  const int64_t bytes = a.n * (a.dtype == SFL_BF16 ? 2 : 4);
+  return a.dtype == b.dtype && (const char*)a.src + bytes == (const char*)b.src && target(a) + bytes == target(b);
+}
+
+// Fills l with the ranges of tensors from list[i] on (from the list's end where `back`) and moves i
+// past them; returns the launch's workgroups.
 int64_t next_launch(const sfl_grad_t* list, int n, bool back, int64_t share, int* i, GradList* l) {
-  int begin = *i, end = *i, held = 0;
-  int64_t blocks = 0;
+  int begin = *i, end = *i, ranges = 0, last = -1;
+  int64_t closed = 0, open = 0;  // workgroups of the ranges before the last one, elements of that
   for (; *i < n; ++*i) {
-    const int64_t c = cdiv(list[back ? n - 1 - *i : *i].n, share);
-    if (held + (c > 0) > kListMax || blocks + c > INT32_MAX) break;
-    held += c > 0;
-    blocks += c;
+    const int at = back ? n - 1 - *i : *i;
+    const int64_t len = list[at].n;
+    if (len > 0) {
+      const bool joins = last >= 0 && (back ? follows(list[at], list[last]) : follows(list[last], list[at]));
+      const int64_t c = joins ? closed : closed + cdiv(open, share), o = joins ? open + len : len;
+      if (ranges + !joins > kListMax || c + cdiv(o, share) > INT32_MAX) break;
+      ranges += !joins;
+      closed = c;
+      open = o;
+      last = at;
+    }
     end = *i + 1;
   }
   if (back) {
@@ -162,21 +178,28 @@ int64_t next_launch(const sfl_grad_t* list, int n, bool back, int64_t share, int
   l->count = 0;
   l->share = (int32_t)share;
   l->first[0] = 0;
+  last = -1;
   for (int j = begin; j < end; ++j) {
-    const int64_t c = cdiv(list[j].n, share);
-    if (c == 0) continue;
-    const int m = l->count++;
-    l->src[m] = list[j].src;
-    l->dst[m] = list[j].dst ? list[j].dst : const_cast<void*>(list[j].src);
-    l->n[m] = list[j].n;
-    l->bf16[m] = list[j].dtype == SFL_BF16;
-    l->first[m + 1] = l->first[m] + (int32_t)c;
+    if (list[j].n == 0) continue;
+    if (last >= 0 && follows(list[last], list[j])) {
+      l->n[l->count - 1] += list[j].n;
+    } else {
+      const int m = l->count++;
+      l->src[m] = list[j].src;
+      l->dst[m] = (void*)target(list[j]);
+      l->n[m] = list[j].n;
+      l->bf16[m] = list[j].dtype == SFL_BF16;
+    }
+    last = j;
+    const int m = l->count - 1;
+    l->first[m + 1] = l->first[m] + (int32_t)cdiv(l->n[m], share);
   }
-  return blocks;
+  return l->first[l->count];
 }
 
 }  // namespace
 
+// A sum per workgroup; ranges of several tensors have at most as many as their tensors alone.
 size_t grad_workspace_bytes(const sfl_grad_t* list, int n) {
   const int64_t share = share_of(elements(list, n), kSumShare);
   int64_t blocks = 0;
