@@ -89,7 +89,7 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
   // every thread of a workgroup takes as many turns (row_sum has barriers)
   for (int64_t t0 = (int64_t)blockIdx.x * L::R; t0 < p.T; t0 += step) {
     const int64_t t = t0 + threadIdx.x / NT;
-    const bool in = t < p.T;
+    const bool in = L::R == 1 || t < p.T;
     const int64_t base = (in ? t : p.T - 1) * p.d;
     Vec8<V> X[CH], Y[CH];
 #pragma unroll
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_bwd(NormBwdParams p
   const int64_t step = (int64_t)gridDim.x * L::R;
   for (int64_t t0 = (int64_t)blockIdx.x * L::R; t0 < p.T; t0 += step) {
     const int64_t t = t0 + threadIdx.x / NT;
-    const bool in = t < p.T;
+    const bool in = L::R == 1 || t < p.T;  // a group past the end goes along (barriers) and adds nothing
     const int64_t base = (in ? t : p.T - 1) * p.d;
     auto load = [&](int i) {
       const int c = (i * NT + x) * kVec, h = i % H;
@@ -208,10 +208,10 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_bwd(NormBwdParams p
     const float k = rx * rx * rx * (s[1] * inv_d);  // D = dX' + rx g - k x
     const float ry = p.post ? 1.f / sqrtf(s[2] * inv_d + p.eps) : 1.f;
     const float Q = ry * (s[3] + rx * s[4] - k * s[5]);
-    const float gt = in ? (p.gate_t ? p.gate_t[t] : 1.f) : 0.f;
-    if (p.dgate_t && in && x == 0) p.dgate_t[t] = Q;
+    if (!in) continue;
+    const float gt = p.gate_t ? p.gate_t[t] : 1.f;
+    if (p.dgate_t && x == 0) p.dgate_t[t] = Q;
     const float gr = gt * ry, ky = p.post ? gr * ry * Q * inv_d : 0.f;  // dY = gr u D - ky y
-    const float xa = in ? rx : 0.f;                                     // rows past the end add nothing
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       if (!HOLD) {
@@ -226,13 +226,13 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_bwd(NormBwdParams p
       for (int e = 0; e < kVec; ++e) {
         const float xv = X[h].get(e), yv = Y[h].get(e), n = N[h].get(e);
         const float D = fmaf(-k, xv, fmaf(rx, n * w[h][e], G[h].get(e)));
-        a[e] = fmaf(n, xv * xa, a[e]);
+        a[e] = fmaf(n, xv * rx, a[e]);
         b[e] = fmaf(D, yv * gr, b[e]);
         dx[e] = p.res_scale * D;
         dy[e] = fmaf(gr * u[h][e], D, -ky * yv);
       }
-      if (p.dX && in) store8((V*)p.dX + base, c, d, dx);
-      if (p.dY && in) store8((V*)p.dY + base, c, d, dy);
+      if (p.dX) store8((V*)p.dX + base, c, d, dx);
+      if (p.dY) store8((V*)p.dY + base, c, d, dy);
     }
   }
   if (!p.part) return;
