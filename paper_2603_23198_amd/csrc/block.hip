@@ -21,32 +21,39 @@ namespace sfl {
 
 namespace {
 
-// Layout of a launch: NT threads per row, each with CH chunks of 8 columns, chunk i of thread x at
-// column (i NT + x) 8; R rows at a time per workgroup. A thread sees the same columns in all of
-// its rows, so it loads their weights once and keeps their parameter sums in registers.
+// Layout of a launch: rows of up to 512 columns take NT = 8 to 64 threads, R = 256 / NT rows at a
+// time per workgroup; wider ones a workgroup of as many waves as they need, at most NT threads.
+// Every thread has CH chunks of 8 columns, chunk i of thread x at column (i NT + x) 8. It sees the
+// same columns in all of its rows, so it loads their weights once and keeps their parameter sums in
+// registers.
 template <int NT> struct Rows {
-  static constexpr int kThreads = NT < 256 ? 256 : NT;
+  static constexpr int kThreads = NT <= kWave ? 256 : NT;
   static constexpr int R = kThreads / NT;
 };
 
-// Sums of n values over the NT threads of a row, in each of them. Above a wave they go through
-// LDS, two buffers in turn (one barrier per call); every wave reads the waves' sums back one per
-// lane and folds them by DPP.
+// Sums of n values over the threads of a row, in each of them. Above a wave they go through LDS, two
+// buffers in turn (one barrier per call); every wave reads the waves' sums back one per lane and
+// folds them by DPP.
 template <int NT, int n> struct RowSum {
   static constexpr int kWaves = NT > kWave ? NT / kWave : 1;
-  float (*buf)[Rows<NT>::R][kWaves][n];
+  float (*buf)[kWaves][n];
   int turn = 0;
+  // waves that the workgroup does not have add zeros; a barrier follows before the sums are read
+  __device__ __forceinline__ RowSum(float (*b)[kWaves][n]) : buf(b) {
+    if (kWaves > 1 && threadIdx.x < kWave)
+      for (int i = threadIdx.x; i < 2 * kWaves * n; i += kWave)
+        if (i / n % kWaves >= (int)blockDim.x / kWave) (&b[0][0][0])[i] = 0.f;
+  }
   __device__ __forceinline__ void operator()(float (&v)[n]) {
 #pragma unroll
     for (int i = 0; i < n; ++i) v[i] = group_sum<(NT < kWave ? NT : kWave)>(v[i]);
     if (NT <= kWave) return;
     if (lane_id() == 0)
 #pragma unroll
-      for (int i = 0; i < n; ++i) buf[turn][threadIdx.x / NT][threadIdx.x % NT / kWave][i] = v[i];
+      for (int i = 0; i < n; ++i) buf[turn][threadIdx.x / kWave][i] = v[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < n; ++i)
-      v[i] = group_sum<(kWaves > 1 ? kWaves : 2)>(buf[turn][threadIdx.x / NT][lane_id() % kWaves][i]);
+    for (int i = 0; i < n; ++i) v[i] = group_sum<(kWaves > 1 ? kWaves : 2)>(buf[turn][lane_id() % kWaves][i]);
     turn ^= 1;
   }
 };
@@ -75,9 +82,9 @@ template <typename P> __device__ __forceinline__ void load_u(const P& p, int c, 
 template <typename V, int NT, int CH>
 __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
   using L = Rows<NT>;
-  __shared__ float red[2][L::R][RowSum<NT, 1>::kWaves][1];
-  RowSum<NT, 1> row_sum{red};
-  const int x = threadIdx.x % NT, d = (int)p.d;
+  __shared__ float red[2][RowSum<NT, 1>::kWaves][1];
+  RowSum<NT, 1> row_sum(red);
+  const int x = NT <= kWave ? threadIdx.x % NT : threadIdx.x, d = (int)p.d;
   const float inv_d = 1.f / (float)d;
   float u[CH][kVec], w[CH][kVec];
 #pragma unroll
@@ -88,7 +95,7 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
   const int64_t step = (int64_t)gridDim.x * L::R;
   // every thread of a workgroup takes as many turns (row_sum has barriers)
   for (int64_t t0 = (int64_t)blockIdx.x * L::R; t0 < p.T; t0 += step) {
-    const int64_t t = t0 + threadIdx.x / NT;
+    const int64_t t = t0 + (L::R == 1 ? 0 : threadIdx.x / NT);
     const bool in = L::R == 1 || t < p.T;
     const int64_t base = (in ? t : p.T - 1) * p.d;
     Vec8<V> X[CH], Y[CH];
@@ -106,7 +113,7 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
 #pragma unroll
         for (int e = 0; e < kVec; ++e) s[0] = fmaf(Y[i].get(e), Y[i].get(e), s[0]);
       row_sum(s);
-      gt *= 1.f / sqrtf(s[0] * inv_d + p.eps);
+      gt *= rsqrtf(s[0] * inv_d + p.eps);
     }
     float o[CH][kVec], s[1] = {0.f};
 #pragma unroll
@@ -122,7 +129,7 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
       for (int i = 0; i < CH; ++i) store8((V*)p.X_out + base, (i * NT + x) * kVec, d, o[i]);
     if (p.pre) {
       row_sum(s);
-      const float rx = 1.f / sqrtf(s[0] * inv_d + p.eps);
+      const float rx = rsqrtf(s[0] * inv_d + p.eps);
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
 #pragma unroll
@@ -136,124 +143,141 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
 // One pass per row: every sum that the outputs need is a sum over the row of products of the loaded
 // values, so all six are taken together (one barrier per row). With q = sum g x, D is
 // dX' + r_x g - r_x^3 q / d x, and the sum of u D y follows from those of u y dX', u y g, u y x.
-// HOLD: the row and the weights stay in registers between the sums and the outputs; else (wide
-// rows) they are read again, from L2, and the parameter sums are kept in LDS.
-template <typename V, int NT, int CH, bool HOLD>
-__global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_bwd(NormBwdParams p) {
-  using L = Rows<NT>;
-  constexpr int H = HOLD ? CH : 1;
-  constexpr int W = CH * NT * kVec;
-  extern __shared__ float sums[];  // [R][2][W], with HOLD only used at the end
-  __shared__ float red[2][L::R][RowSum<NT, 6>::kWaves][6];
-  RowSum<NT, 6> row_sum{red};
-  const int x = threadIdx.x % NT, d = (int)p.d;
-  const float inv_d = 1.f / (float)d;
-  float u[H][kVec], w[H][kVec], A[H][kVec], S[H][kVec];
-  float* mine = sums + threadIdx.x / NT * 2 * W + x * kVec;  // chunk i of A at i NT 8, of S at W + i NT 8
-#pragma unroll
-  for (int i = 0; i < CH; ++i) {
-    if (HOLD) {
-      load_u(p, (i * NT + x) * kVec, d, u[i % H]);
-      load_param(p.w_pre, (i * NT + x) * kVec, d, w[i % H]);
-    }
+// HOLD: the row, the weights and the parameter sums stay in registers; else (wide rows) the row and
+// the weights are read again, from L2, for the outputs, and the sums are kept in LDS.
+// A bf16 row's loads go out while the row before it is still being summed (16 registers; fp32 rows
+// have twice the bytes in flight without).
+template <typename V> struct BwdRow {
+  Vec8<V> X, Y, G, N;  // X_out, Y, dX_out, dN
+  __device__ __forceinline__ void load(const NormBwdParams& p, int64_t base, int c, int d) {
+    X = p.pre ? load8((const V*)p.X_out + base, c, d) : Vec8<V>{};
+    Y = p.Y ? load8((const V*)p.Y + base, c, d) : Vec8<V>{};
+    G = p.dX_out ? load8((const V*)p.dX_out + base, c, d) : Vec8<V>{};
+    N = p.dN ? load8((const V*)p.dN + base, c, d) : Vec8<V>{};
+  }
+  __device__ __forceinline__ void add_to(float (&s)[6], const float (&u)[kVec], const float (&w)[kVec]) const {
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
-      if (HOLD)
-        A[i % H][e] = S[i % H][e] = 0.f;
-      else
-        mine[i * NT * kVec + e] = mine[W + i * NT * kVec + e] = 0.f;
+      const float xv = X.get(e), yv = Y.get(e), g = N.get(e) * w[e], uy = u[e] * yv;
+      s[0] = fmaf(xv, xv, s[0]);
+      s[1] = fmaf(g, xv, s[1]);
+      s[2] = fmaf(yv, yv, s[2]);
+      s[3] = fmaf(uy, G.get(e), s[3]);
+      s[4] = fmaf(uy, g, s[4]);
+      s[5] = fmaf(uy, xv, s[5]);
     }
   }
-  Vec8<V> X[H], Y[H], G[H], N[H];  // X_out, Y, dX_out, dN
+};
+
+// What the outputs of a row take from its sums.
+struct BwdCoef {
+  float rx, k, gr, ky, Q;  // D = dX' + rx g - k x, dY = gr u D - ky y
+  __device__ __forceinline__ BwdCoef(const NormBwdParams& p, const float (&s)[6], float inv_d, float gt) {
+    rx = p.pre ? rsqrtf(s[0] * inv_d + p.eps) : 0.f;
+    k = rx * rx * rx * (s[1] * inv_d);
+    const float ry = p.post ? rsqrtf(s[2] * inv_d + p.eps) : 1.f;
+    Q = ry * (s[3] + rx * s[4] - k * s[5]);
+    gr = gt * ry;
+    ky = p.post ? gr * ry * Q * inv_d : 0.f;
+  }
+  template <typename V, typename F>
+  __device__ __forceinline__ void outputs(const NormBwdParams& p, const BwdRow<V>& r, const float (&u)[kVec],
+                                          const float (&w)[kVec], F* A, F* S, int64_t base, int c, int d) const {
+    float dx[kVec], dy[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      const float xv = r.X.get(e), yv = r.Y.get(e), n = r.N.get(e);
+      const float D = fmaf(-k, xv, fmaf(rx, n * w[e], r.G.get(e)));
+      A[e] = fmaf(n, xv * rx, A[e]);
+      S[e] = fmaf(D, yv * gr, S[e]);
+      dx[e] = p.res_scale * D;
+      dy[e] = fmaf(gr * u[e], D, -ky * yv);
+    }
+    if (p.dX) store8((V*)p.dX + base, c, d, dx);
+    if (p.dY) store8((V*)p.dY + base, c, d, dy);
+  }
+};
+
+template <typename V, int NT, int CH, bool HOLD>
+__global__ __launch_bounds__(Rows<NT>::kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))) void k_norm_bwd(NormBwdParams p) {
+  static_assert(!HOLD || CH == 1, "");
+  using L = Rows<NT>;
+  constexpr bool AHEAD = HOLD && sizeof(V) == 2;
+  extern __shared__ float sums[];  // [R][2][CH * NT * 8]: A, S; with HOLD used at the end where R > 1
+  __shared__ float red[2][RowSum<NT, 6>::kWaves][6];
+  RowSum<NT, 6> row_sum(red);
+  constexpr int W = CH * NT * kVec;
+  const int x = NT <= kWave ? threadIdx.x % NT : threadIdx.x, d = (int)p.d, group = L::R == 1 ? 0 : threadIdx.x / NT;
+  const float inv_d = 1.f / (float)d;
+  float* mine = sums + group * 2 * W + x * kVec;  // chunk i at i NT 8, S behind A
+  float u[kVec], w[kVec], A[kVec], S[kVec];
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) A[e] = S[e] = 0.f;
+  if (HOLD) {
+    load_u(p, x * kVec, d, u);
+    load_param(p.w_pre, x * kVec, d, w);
+  } else {
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) mine[i * NT * kVec + e] = mine[W + i * NT * kVec + e] = 0.f;
+  }
   const int64_t step = (int64_t)gridDim.x * L::R;
+  auto row_of = [&](int64_t t0) { return L::R == 1 ? t0 : min(t0 + group, p.T - 1); };
+  BwdRow<V> now, next;
+  if (AHEAD) next.load(p, row_of((int64_t)blockIdx.x * L::R) * p.d, x * kVec, d);
   for (int64_t t0 = (int64_t)blockIdx.x * L::R; t0 < p.T; t0 += step) {
-    const int64_t t = t0 + threadIdx.x / NT;
-    const bool in = L::R == 1 || t < p.T;  // a group past the end goes along (barriers) and adds nothing
-    const int64_t base = (in ? t : p.T - 1) * p.d;
-    auto load = [&](int i) {
-      const int c = (i * NT + x) * kVec, h = i % H;
-      X[h] = p.pre ? load8((const V*)p.X_out + base, c, d) : Vec8<V>{};
-      Y[h] = p.Y ? load8((const V*)p.Y + base, c, d) : Vec8<V>{};
-      G[h] = p.dX_out ? load8((const V*)p.dX_out + base, c, d) : Vec8<V>{};
-      N[h] = p.dN ? load8((const V*)p.dN + base, c, d) : Vec8<V>{};
-      if (!HOLD) {
-        load_u(p, c, d, u[0]);
-        load_param(p.w_pre, c, d, w[0]);
-      }
-    };
-    if (HOLD)
-#pragma unroll
-      for (int i = 0; i < CH; ++i) load(i);
+    const int64_t t = row_of(t0), base = t * p.d;
+    const bool in = L::R == 1 || t0 + group < p.T;  // a group past the end goes along (barriers) and adds nothing
     float s[6] = {};
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      if (!HOLD) {
-        __builtin_amdgcn_sched_barrier(0);  // one chunk's registers at a time
-        load(i);
-      }
-      const int h = i % H;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float xv = X[h].get(e), yv = Y[h].get(e), g = N[h].get(e) * w[h][e], uy = u[h][e] * yv;
-        s[0] = fmaf(xv, xv, s[0]);
-        s[1] = fmaf(g, xv, s[1]);
-        s[2] = fmaf(yv, yv, s[2]);
-        s[3] = fmaf(uy, G[h].get(e), s[3]);
-        s[4] = fmaf(uy, g, s[4]);
-        s[5] = fmaf(uy, xv, s[5]);
+    if (HOLD) {
+      if (AHEAD)
+        now = next;
+      else
+        now.load(p, base, x * kVec, d);
+      now.add_to(s, u, w);
+      if (AHEAD && t0 + step < p.T) next.load(p, row_of(t0 + step) * p.d, x * kVec, d);
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < CH; ++i) {
+        const int c = (i * NT + x) * kVec;
+        now.load(p, base, c, d);
+        load_u(p, c, d, u);
+        load_param(p.w_pre, c, d, w);
+        now.add_to(s, u, w);
       }
     }
     row_sum(s);
-    const float rx = p.pre ? 1.f / sqrtf(s[0] * inv_d + p.eps) : 0.f;
-    const float k = rx * rx * rx * (s[1] * inv_d);  // D = dX' + rx g - k x
-    const float ry = p.post ? 1.f / sqrtf(s[2] * inv_d + p.eps) : 1.f;
-    const float Q = ry * (s[3] + rx * s[4] - k * s[5]);
     if (!in) continue;
-    const float gt = p.gate_t ? p.gate_t[t] : 1.f;
-    if (p.dgate_t && x == 0) p.dgate_t[t] = Q;
-    const float gr = gt * ry, ky = p.post ? gr * ry * Q * inv_d : 0.f;  // dY = gr u D - ky y
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      if (!HOLD) {
-        __builtin_amdgcn_sched_barrier(0);
-        load(i);
+    const BwdCoef f(p, s, inv_d, p.gate_t ? p.gate_t[t] : 1.f);
+    if (p.dgate_t && x == 0) p.dgate_t[t] = f.Q;
+    if (HOLD) {
+      f.outputs(p, now, u, w, A, S, base, x * kVec, d);
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < CH; ++i) {
+        const int c = (i * NT + x) * kVec;
+        now.load(p, base, c, d);
+        load_u(p, c, d, u);
+        load_param(p.w_pre, c, d, w);
+        f.outputs(p, now, u, w, mine + i * NT * kVec, mine + W + i * NT * kVec, base, c, d);
       }
-      const int h = i % H, c = (i * NT + x) * kVec;
-      float dx[kVec], dy[kVec];
-      float(&a)[kVec] = HOLD ? A[h] : *(float(*)[kVec])(mine + i * NT * kVec);
-      float(&b)[kVec] = HOLD ? S[h] : *(float(*)[kVec])(mine + W + i * NT * kVec);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float xv = X[h].get(e), yv = Y[h].get(e), n = N[h].get(e);
-        const float D = fmaf(-k, xv, fmaf(rx, n * w[h][e], G[h].get(e)));
-        a[e] = fmaf(n, xv * rx, a[e]);
-        b[e] = fmaf(D, yv * gr, b[e]);
-        dx[e] = p.res_scale * D;
-        dy[e] = fmaf(gr * u[h][e], D, -ky * yv);
-      }
-      if (p.dX) store8((V*)p.dX + base, c, d, dx);
-      if (p.dY) store8((V*)p.dY + base, c, d, dy);
     }
   }
   if (!p.part) return;
   float* part = p.part + (int64_t)blockIdx.x * 2 * d;
   if (HOLD && L::R == 1) {
-#pragma unroll
-    for (int i = 0; i < H; ++i) {
-      store8(part, (i * NT + x) * kVec, d, A[i]);
-      store8(part + d, (i * NT + x) * kVec, d, S[i]);
-    }
+    store8(part, x * kVec, d, A);
+    store8(part + d, x * kVec, d, S);
     return;
   }
   // the workgroup's R rows at a time, added in row order
   if (HOLD)
 #pragma unroll
-    for (int i = 0; i < H; ++i)
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        mine[i * NT * kVec + e] = A[i][e];
-        mine[W + i * NT * kVec + e] = S[i][e];
-      }
+    for (int e = 0; e < kVec; ++e) {
+      mine[e] = A[e];
+      mine[W + e] = S[e];
+    }
   __syncthreads();
   for (int j = threadIdx.x; j < 2 * W; j += L::kThreads) {
     float v = 0.f;
@@ -300,27 +324,32 @@ __global__ __launch_bounds__(kSumThreads) void k_norm_param_sums(NormBwdParams p
   }
 }
 
-// Workgroups of the backward: what the chip holds at a time, so that each adds up as many rows as
-// can be before it leaves its sums.
-constexpr int kBwdBlocks = 512;
-
-// Calls f with NT and CH for a width: one chunk per thread up to 8192 columns, then two.
+// Calls f with NT, CH and the threads of a workgroup for a width: one chunk per thread up to 8192
+// columns, then two.
 template <typename F> hipError_t with_layout(int64_t d, F f) {
   using std::integral_constant;
   const int64_t n = cdiv(d, kVec);
+  const int threads = (int)std::min<int64_t>(cdiv(n, kWave) * kWave, 1024);
 #define SFL_NT(nt) \
-  if (n <= nt) return f(integral_constant<int, nt>{}, integral_constant<int, 1>{});
+  if (n <= nt) return f(integral_constant<int, nt>{}, integral_constant<int, 1>{}, nt <= kWave ? 256 : threads);
   SFL_NT(8) SFL_NT(16) SFL_NT(32) SFL_NT(64) SFL_NT(128) SFL_NT(256) SFL_NT(512) SFL_NT(1024)
 #undef SFL_NT
-  return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+  return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{}, threads);
 }
 
 }  // namespace
 
+// Workgroups of the backward. The fewer there are, the more rows each adds up before it leaves its
+// sums, so a CU gets the twelve waves that keep the memory busy with full loads, or all sixteen that
+// its registers hold where rows leave lanes idle or are not whole in 16-byte units (bf16 d = 4096: 81
+// us with twelve waves, 89 with sixteen; d = 640: 139 and 119; d = 1003: 154 and 138).
 static int64_t bwd_blocks(int64_t T, int64_t d) {
   int64_t blocks = 0;
-  (void)with_layout(d, [&](auto nt, auto) {
-    blocks = std::min<int64_t>(cdiv(T, Rows<decltype(nt)::value>::R), kBwdBlocks);
+  (void)with_layout(d, [&](auto nt, auto, int threads) {
+    constexpr int NT = decltype(nt)::value;
+    const int64_t chunks = cdiv(d, kVec), lanes = NT <= kWave ? NT : threads;
+    const int waves = d % kVec == 0 && 4 * chunks >= 3 * lanes ? 12 : 16;
+    blocks = std::min<int64_t>(cdiv(T, Rows<NT>::R), 256 * std::max(1, waves * kWave / threads));
     return hipSuccess;
   });
   return blocks;
@@ -329,16 +358,16 @@ static int64_t bwd_blocks(int64_t T, int64_t d) {
 size_t norm_workspace_bytes(int64_t T, int64_t d) { return (size_t)bwd_blocks(T, d) * 2 * (size_t)d * sizeof(float); }
 
 hipError_t launch_norm_fwd(const NormParams& p, int bf16, hipStream_t s) {
-  return with_layout(p.d, [&](auto nt, auto ch) {
+  return with_layout(p.d, [&](auto nt, auto ch, int threads) {
     constexpr int NT = decltype(nt)::value, CH = decltype(ch)::value;
     using L = Rows<NT>;
     // twice what the chip holds at a time: rows of a second round fill in where the first's end
     // (8192 x 4096 bf16: 60 us with one round, 56 with two, 64 with a workgroup per row)
-    const unsigned grid = (unsigned)std::min<int64_t>(cdiv(p.T, L::R), 256 * (4096 / L::kThreads));
+    const unsigned grid = (unsigned)std::min<int64_t>(cdiv(p.T, L::R), 256 * (4096 / threads));
     if (bf16)
-      hipLaunchKernelGGL((k_norm_fwd<bf16_t, NT, CH>), dim3(grid), dim3(L::kThreads), 0, s, p);
+      hipLaunchKernelGGL((k_norm_fwd<bf16_t, NT, CH>), dim3(grid), dim3(threads), 0, s, p);
     else
-      hipLaunchKernelGGL((k_norm_fwd<float, NT, CH>), dim3(grid), dim3(L::kThreads), 0, s, p);
+      hipLaunchKernelGGL((k_norm_fwd<float, NT, CH>), dim3(grid), dim3(threads), 0, s, p);
     return hipGetLastError();
   });
 }
@@ -348,7 +377,7 @@ hipError_t launch_norm_bwd(const NormBwdParams& p0, int bf16, hipStream_t s) {
   const int64_t blocks = bwd_blocks(p.T, p.d);
   if (!p.dw_pre && !p.dw_post && !p.dgate_c) p.part = nullptr;
   if (blocks > 0) {
-    const hipError_t e = with_layout(p.d, [&](auto nt, auto ch) {
+    const hipError_t e = with_layout(p.d, [&](auto nt, auto ch, int threads) {
       constexpr int NT = decltype(nt)::value, CH = decltype(ch)::value;
       using L = Rows<NT>;
       constexpr bool HOLD = CH == 1;
@@ -359,7 +388,7 @@ hipError_t launch_norm_bwd(const NormBwdParams& p0, int bf16, hipStream_t s) {
             hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
       }
-      hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(L::kThreads), lds, s, p);
+      hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(threads), lds, s, p);
       return hipGetLastError();
     });
     if (e != hipSuccess) return e;

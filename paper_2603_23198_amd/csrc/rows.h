@@ -39,62 +39,97 @@ template <typename T, typename P> __device__ __forceinline__ void store16(P* p, 
 __device__ __forceinline__ Vec8<bf16_t> load_full(const bf16_t* p) { return {load16<u32x4_t>(p)}; }
 __device__ __forceinline__ Vec8<float> load_full(const float* p) { return {load16<f32x4_t>(p), load16<f32x4_t>(p + 4)}; }
 
-// Elements c .. c + 7 of a row of d; zeros past its end.
+// Drops the first s of eight elements and lets zeros in behind them.
+__device__ __forceinline__ void drop(Vec8<bf16_t>& v, int s) {
+  uint64_t lo = (uint64_t)v.w[1] << 32 | v.w[0], hi = (uint64_t)v.w[3] << 32 | v.w[2];
+  if (s & 4) {
+    lo = hi;
+    hi = 0;
+  }
+  const int bits = (s & 3) * 16;
+  if (bits) {
+    lo = lo >> bits | hi << (64 - bits);
+    hi >>= bits;
+  }
+  v.w = u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+__device__ __forceinline__ void drop(Vec8<float>& v, int s) {
+  if (s & 4) {
+    v.a = v.b;
+    v.b = f32x4_t{};
+  }
+  if (s & 2) {
+    v.a = f32x4_t{v.a[2], v.a[3], v.b[0], v.b[1]};
+    v.b = f32x4_t{v.b[2], v.b[3], 0.f, 0.f};
+  }
+  if (s & 1) {
+    v.a = f32x4_t{v.a[1], v.a[2], v.a[3], v.b[0]};
+    v.b = f32x4_t{v.b[1], v.b[2], v.b[3], 0.f};
+  }
+}
+
+// Elements c .. c + 7 of a row of d; zeros past its end. The chunk over the end is the row's last
+// eight elements shifted down.
 template <typename V> __device__ __forceinline__ Vec8<V> load8(const V* row, int c, int d) {
   if (c + kVec <= d) return load_full(row + c);
   Vec8<V> v{};
-  if (c < d) {
-    V e[kVec] = {};
-#pragma unroll
-    for (int i = 0; i < kVec; ++i)
-      if (c + i < d) e[i] = row[c + i];
-    __builtin_memcpy(&v, e, sizeof(e));
+  if (c >= d) return v;
+  if (d >= kVec) {
+    v = load_full(row + d - kVec);
+    drop(v, c + kVec - d);
+    return v;
   }
+  V e[kVec] = {};
+#pragma unroll
+  for (int i = 0; i < kVec; ++i)
+    if (c + i < d) e[i] = row[c + i];
+  __builtin_memcpy(&v, e, sizeof(e));
   return v;
 }
 
-// The same eight elements to another row.
 __device__ __forceinline__ void store_full(bf16_t* p, const Vec8<bf16_t>& v) { store16(p, v.w); }
 __device__ __forceinline__ void store_full(float* p, const Vec8<float>& v) {
   store16(p, v.a);
   store16(p + 4, v.b);
 }
-template <typename V> __device__ __forceinline__ void copy8(V* row, int c, int d, const Vec8<V>& v) {
-  if (c + kVec <= d) {
-    store_full(row + c, v);
-  } else {
-    V e[kVec];
-    __builtin_memcpy(e, &v, sizeof(e));
-#pragma unroll
-    for (int i = 0; i < kVec; ++i)
-      if (c + i < d) row[c + i] = e[i];
+
+// Eight elements to c .. c + 7 of a row of d; what is past its end is left out (four, two and one
+// elements at a time).
+template <typename V> __device__ __forceinline__ void copy8(V* row, int c, int d, Vec8<V> v) {
+  if (c + kVec <= d) return store_full(row + c, v);
+  if (c >= d) return;
+  V* p = row + c;
+  const int left = d - c;
+  if (left & 4) {
+    __builtin_memcpy(p, &v, 4 * sizeof(V));
+    p += 4;
+    drop(v, 4);
   }
+  if (left & 2) {
+    __builtin_memcpy(p, &v, 2 * sizeof(V));
+    p += 2;
+    drop(v, 2);
+  }
+  if (left & 1) __builtin_memcpy(p, &v, sizeof(V));
 }
 
-// Two floats to packed bf16, each to nearest even (NaN stays a NaN).
+// Two floats to packed bf16, each to nearest even (NaN stays a NaN): one v_cvt_pk_bf16_f32.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  return (uint32_t)f32_to_bf16(lo) | (uint32_t)f32_to_bf16(hi) << 16;
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  const bf16x2_t v = __builtin_convertvector((f32x2_t{lo, hi}), bf16x2_t);
+  uint32_t w;
+  __builtin_memcpy(&w, &v, 4);
+  return w;
 }
 
-template <typename V> __device__ __forceinline__ void store8(V* row, int c, int d, const float (&v)[kVec]);
-template <> __device__ __forceinline__ void store8<bf16_t>(bf16_t* row, int c, int d, const float (&v)[kVec]) {
-  if (c + kVec <= d) {
-    store16(row + c, u32x4_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])});
-  } else {
-#pragma unroll
-    for (int i = 0; i < kVec; ++i)
-      if (c + i < d) row[c + i] = f32_to_bf16(v[i]);
-  }
+__device__ __forceinline__ Vec8<bf16_t> rounded(const float (&v)[kVec], bf16_t) {
+  return {u32x4_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])}};
 }
-template <> __device__ __forceinline__ void store8<float>(float* row, int c, int d, const float (&v)[kVec]) {
-  if (c + kVec <= d) {
-    store16(row + c, f32x4_t{v[0], v[1], v[2], v[3]});
-    store16(row + c + 4, f32x4_t{v[4], v[5], v[6], v[7]});
-  } else {
-#pragma unroll
-    for (int i = 0; i < kVec; ++i)
-      if (c + i < d) row[c + i] = v[i];
-  }
+__device__ __forceinline__ Vec8<float> rounded(const float (&v)[kVec], float) {
+  return {f32x4_t{v[0], v[1], v[2], v[3]}, f32x4_t{v[4], v[5], v[6], v[7]}};
+}
+template <typename V> __device__ __forceinline__ void store8(V* row, int c, int d, const float (&v)[kVec]) {
+  copy8(row, c, d, rounded(v, V{}));
 }
 
 template <int CTRL> __device__ __forceinline__ float dpp_add(float v) {
