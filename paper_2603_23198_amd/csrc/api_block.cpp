@@ -91,7 +91,7 @@ sfl_status_t sfl_norm_forward(const sfl_norm_args_t* a, sfl_stream_t stream) {
 sfl_status_t sfl_norm_workspace_size(int64_t T, int64_t d, sfl_dtype_t dtype, size_t* bytes) {
   if (!bytes || !dtype_ok(dtype) || !size_ok(T, d)) return SFL_E_ARG;
   if (d > kNormMaxWidth) return SFL_E_UNSUPPORTED;
-  *bytes = norm_workspace_bytes(T, d);
+  *bytes = norm_workspace_bytes(T, d, dtype == SFL_BF16);
   return SFL_OK;
 }
 
@@ -104,7 +104,7 @@ sfl_status_t sfl_norm_backward(const sfl_norm_bwd_args_t* a, sfl_stream_t stream
   if ((a->dN || a->dw_pre) && !pre) return SFL_E_ARG;
   if (a->dw_post && !post) return SFL_E_ARG;
   if (a->T > 0 && ((pre && !a->X_out) || (!a->Y && (a->dY || a->dgate_c || a->dgate_t)))) return SFL_E_ARG;
-  const size_t need = norm_workspace_bytes(a->T, a->d);
+  const size_t need = norm_workspace_bytes(a->T, a->d, a->dtype == SFL_BF16);
   if (need > 0 && (!a->workspace || a->workspace_bytes < need)) return SFL_E_WORKSPACE;
   NormBwdParams p{};
   p.T = a->T;

@@ -42,11 +42,11 @@ struct NormBwdParams {
   float* dw_post;
   float* dgate_c;
   float* dgate_t;
-  float* part;  // norm_workspace_bytes(T, d)
+  float* part;  // norm_workspace_bytes(T, d, bf16)
   float eps, res_scale;
   int pre, post;
 };
-size_t norm_workspace_bytes(int64_t T, int64_t d);
+size_t norm_workspace_bytes(int64_t T, int64_t d, int bf16);
 hipError_t launch_norm_fwd(const NormParams& p, int bf16, hipStream_t s);
 hipError_t launch_norm_bwd(const NormBwdParams& p, int bf16, hipStream_t s);
 

@@ -102,8 +102,14 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int c = (i * NT + x) * kVec;
-      X[i] = load8((const V*)p.X + base, c, d);
-      if (p.Y) Y[i] = load8((const V*)p.Y + base, c, d);
+      X[i] = load_raw((const V*)p.X + base, c, d);
+      if (p.Y) Y[i] = load_raw((const V*)p.Y + base, c, d);
+    }
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int c = (i * NT + x) * kVec;
+      settle(X[i], c, d);
+      if (p.Y) settle(Y[i], c, d);
     }
     float gt = p.gate_t ? p.gate_t[in ? t : p.T - 1] : 1.f;
     if (p.post) {
@@ -150,10 +156,17 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
 template <typename V> struct BwdRow {
   Vec8<V> X, Y, G, N;  // X_out, Y, dX_out, dN
   __device__ __forceinline__ void load(const NormBwdParams& p, int64_t base, int c, int d) {
-    X = p.pre ? load8((const V*)p.X_out + base, c, d) : Vec8<V>{};
-    Y = p.Y ? load8((const V*)p.Y + base, c, d) : Vec8<V>{};
-    G = p.dX_out ? load8((const V*)p.dX_out + base, c, d) : Vec8<V>{};
-    N = p.dN ? load8((const V*)p.dN + base, c, d) : Vec8<V>{};
+    X = p.pre ? load_raw((const V*)p.X_out + base, c, d) : Vec8<V>{};
+    Y = p.Y ? load_raw((const V*)p.Y + base, c, d) : Vec8<V>{};
+    G = p.dX_out ? load_raw((const V*)p.dX_out + base, c, d) : Vec8<V>{};
+    N = p.dN ? load_raw((const V*)p.dN + base, c, d) : Vec8<V>{};
+  }
+  __device__ __forceinline__ void settled(int c, int d) {
+    if (c + kVec <= d) return;
+    settle(X, c, d);
+    settle(Y, c, d);
+    settle(G, c, d);
+    settle(N, c, d);
   }
   __device__ __forceinline__ void add_to(float (&s)[6], const float (&u)[kVec], const float (&w)[kVec]) const {
 #pragma unroll
@@ -235,6 +248,7 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) __attribute__((amdgpu_waves_per
         now = next;
       else
         now.load(p, base, x * kVec, d);
+      now.settled(x * kVec, d);
       now.add_to(s, u, w);
       if (AHEAD && t0 + step < p.T) next.load(p, row_of(t0 + step) * p.d, x * kVec, d);
     } else {
@@ -242,6 +256,7 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) __attribute__((amdgpu_waves_per
       for (int i = 0; i < CH; ++i) {
         const int c = (i * NT + x) * kVec;
         now.load(p, base, c, d);
+        now.settled(c, d);
         load_u(p, c, d, u);
         load_param(p.w_pre, c, d, w);
         now.add_to(s, u, w);
@@ -258,6 +273,7 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) __attribute__((amdgpu_waves_per
       for (int i = 0; i < CH; ++i) {
         const int c = (i * NT + x) * kVec;
         now.load(p, base, c, d);
+        now.settled(c, d);
         load_u(p, c, d, u);
         load_param(p.w_pre, c, d, w);
         f.outputs(p, now, u, w, mine + i * NT * kVec, mine + W + i * NT * kVec, base, c, d);
@@ -340,22 +356,25 @@ template <typename F> hipError_t with_layout(int64_t d, F f) {
 }  // namespace
 
 // Workgroups of the backward. The fewer there are, the more rows each adds up before it leaves its
-// sums, so a CU gets the twelve waves that keep the memory busy with full loads, or all sixteen that
-// its registers hold where rows leave lanes idle or are not whole in 16-byte units (bf16 d = 4096: 81
-// us with twelve waves, 89 with sixteen; d = 640: 139 and 119; d = 1003: 154 and 138).
-static int64_t bwd_blocks(int64_t T, int64_t d) {
+// sums, so a CU gets the twelve waves (eight of fp32) that keep the memory busy with full loads, or
+// all sixteen that its registers hold where rows leave lanes idle or are not whole in 16-byte units
+// (rows of 2^26 bytes in all, bf16 d = 4096: 81 us with twelve waves, 89 with sixteen; d = 640: 139
+// and 119; fp32 d = 2048: 81 with eight, 90 with twelve).
+static int64_t bwd_blocks(int64_t T, int64_t d, int bf16) {
   int64_t blocks = 0;
   (void)with_layout(d, [&](auto nt, auto, int threads) {
     constexpr int NT = decltype(nt)::value;
     const int64_t chunks = cdiv(d, kVec), lanes = NT <= kWave ? NT : threads;
-    const int waves = d % kVec == 0 && 4 * chunks >= 3 * lanes ? 12 : 16;
+    const int waves = d % kVec == 0 && 4 * chunks >= 3 * lanes ? (bf16 ? 12 : 8) : 16;
     blocks = std::min<int64_t>(cdiv(T, Rows<NT>::R), 256 * std::max(1, waves * kWave / threads));
     return hipSuccess;
   });
   return blocks;
 }
 
-size_t norm_workspace_bytes(int64_t T, int64_t d) { return (size_t)bwd_blocks(T, d) * 2 * (size_t)d * sizeof(float); }
+size_t norm_workspace_bytes(int64_t T, int64_t d, int bf16) {
+  return (size_t)bwd_blocks(T, d, bf16) * 2 * (size_t)d * sizeof(float);
+}
 
 hipError_t launch_norm_fwd(const NormParams& p, int bf16, hipStream_t s) {
   return with_layout(p.d, [&](auto nt, auto ch, int threads) {
@@ -374,7 +393,7 @@ hipError_t launch_norm_fwd(const NormParams& p, int bf16, hipStream_t s) {
 
 hipError_t launch_norm_bwd(const NormBwdParams& p0, int bf16, hipStream_t s) {
   NormBwdParams p = p0;
-  const int64_t blocks = bwd_blocks(p.T, p.d);
+  const int64_t blocks = bwd_blocks(p.T, p.d, bf16);
   if (!p.dw_pre && !p.dw_post && !p.dgate_c) p.part = nullptr;
   if (blocks > 0) {
     const hipError_t e = with_layout(p.d, [&](auto nt, auto ch, int threads) {

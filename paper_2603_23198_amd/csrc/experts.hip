@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void k_expert_small(const int32_t* __rest
   Vec8<V> v[2];
   if (X)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) v[i] = load8(from, c0 + i * kStep, (int)d);
+    for (int i = 0; i < 2; ++i) v[i] = load_raw(from, c0 + i * kStep, (int)d);
   int mine[kSmallPer];
 #pragma unroll
   for (int i = 0; i < kSmallPer; ++i) {
@@ -130,12 +130,12 @@ __global__ __launch_bounds__(kThreads) void k_expert_small(const int32_t* __rest
   for (int64_t c = c0; c < d; c += 2 * kStep) {
     if (c != c0)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) v[i] = load8(from, (int)c + i * kStep, (int)d);
+      for (int i = 0; i < 2; ++i) v[i] = load_raw(from, (int)c + i * kStep, (int)d);
     for (int j = 0; j < k; ++j) {
       const int p = cnt[kRouteMaxK * W + j];
       if (p >= 0 && p < rows)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) copy8(Xs + p * d, (int)c + i * kStep, (int)d, v[i]);
+        for (int i = 0; i < 2; ++i) store_raw(Xs + p * d, (int)c + i * kStep, (int)d, v[i]);
     }
   }
 }
@@ -242,12 +242,12 @@ __global__ __launch_bounds__(kThreads) void k_expert_rows(const V* __restrict__ 
   for (int c = threadIdx.x % NT * kVec; c < d; c += kRowChunks * NT * kVec) {
     Vec8<V> v[kRowChunks];
 #pragma unroll
-    for (int i = 0; i < kRowChunks; ++i) v[i] = load8(from, c + i * NT * kVec, d);
+    for (int i = 0; i < kRowChunks; ++i) v[i] = load_raw(from, c + i * NT * kVec, d);
     for (int j = 0; j < k; ++j) {
       const int p = pos[t * k + j];
       if (p >= 0 && p < rows)
 #pragma unroll
-        for (int i = 0; i < kRowChunks; ++i) copy8(Xs + p * d64, c + i * NT * kVec, d, v[i]);
+        for (int i = 0; i < kRowChunks; ++i) store_raw(Xs + p * d64, c + i * NT * kVec, d, v[i]);
     }
   }
 }
@@ -274,7 +274,7 @@ __global__ __launch_bounds__(kThreads) void k_expert_combine(const V* __restrict
         const int p = pos[slot];
         in[j] = j0 + j < k && p >= 0 && p < rows;
         w[j] = weight ? weight[slot] : 1.f;
-        if (in[j]) v[j] = load8(Ys + p * d64, c, d);
+        if (in[j]) v[j] = load_raw(Ys + p * d64, c, d);
       }
 #pragma unroll
       for (int j = 0; j < KS; ++j)
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(kThreads) void k_expert_combine(const V* __restrict
 #pragma unroll
           for (int e = 0; e < kVec; ++e) s[e] = fmaf(w[j], v[j].get(e), s[e]);
     }
-    store8(Y + t * d64, c, d, s);
+    store8_raw(Y + t * d64, c, d, s);
   }
 }
 
@@ -312,23 +312,30 @@ __global__ __launch_bounds__(kThreads) void k_expert_combine_bwd(const V* __rest
       dot[j] = 0.f;
     }
     for (int c = threadIdx.x % NT * kVec; c < d; c += NT * kVec) {
-      const Vec8<V> g = load8(dY + t * d64, c, d);
+      const Vec8<V> g = load_raw(dY + t * d64, c, d);
+      const int skip = raw_overlap(c, d);  // these count in the neighbour's dot product
       Vec8<V> v[KS];
       if (dweight)
 #pragma unroll
         for (int j = 0; j < KS; ++j)
-          if (p[j] >= 0) v[j] = load8(Ys + p[j] * d64, c, d);
+          if (p[j] >= 0) v[j] = load_raw(Ys + p[j] * d64, c, d);
 #pragma unroll
       for (int j = 0; j < KS; ++j) {
         if (p[j] < 0) continue;
-        if (dweight)
+        if (dweight) {
+          if (skip == 0) {
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) dot[j] = fmaf(g.get(e), v[j].get(e), dot[j]);
+            for (int e = 0; e < kVec; ++e) dot[j] = fmaf(g.get(e), v[j].get(e), dot[j]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) dot[j] = e < skip ? dot[j] : fmaf(g.get(e), v[j].get(e), dot[j]);
+          }
+        }
         if (dYs) {
           float o[kVec];
 #pragma unroll
           for (int e = 0; e < kVec; ++e) o[e] = w[j] * g.get(e);
-          store8(dYs + p[j] * d64, c, d, o);
+          store8_raw(dYs + p[j] * d64, c, d, o);
         }
       }
     }

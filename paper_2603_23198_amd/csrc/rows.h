@@ -39,7 +39,7 @@ template <typename T, typename P> __device__ __forceinline__ void store16(P* p, 
 __device__ __forceinline__ Vec8<bf16_t> load_full(const bf16_t* p) { return {load16<u32x4_t>(p)}; }
 __device__ __forceinline__ Vec8<float> load_full(const float* p) { return {load16<f32x4_t>(p), load16<f32x4_t>(p + 4)}; }
 
-// Drops the first s of eight elements and lets zeros in behind them.
+// Drops the first s <= 8 of eight elements and lets zeros in behind them.
 __device__ __forceinline__ void drop(Vec8<bf16_t>& v, int s) {
   uint64_t lo = (uint64_t)v.w[1] << 32 | v.w[0], hi = (uint64_t)v.w[3] << 32 | v.w[2];
   if (s & 4) {
@@ -51,6 +51,7 @@ __device__ __forceinline__ void drop(Vec8<bf16_t>& v, int s) {
     lo = lo >> bits | hi << (64 - bits);
     hi >>= bits;
   }
+  if (s & 8) lo = hi = 0;
   v.w = u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
 __device__ __forceinline__ void drop(Vec8<float>& v, int s) {
@@ -66,24 +67,29 @@ __device__ __forceinline__ void drop(Vec8<float>& v, int s) {
     v.a = f32x4_t{v.a[1], v.a[2], v.a[3], v.b[0]};
     v.b = f32x4_t{v.b[1], v.b[2], v.b[3], 0.f};
   }
+  if (s & 8) v.a = v.b = f32x4_t{};
 }
 
-// Elements c .. c + 7 of a row of d; zeros past its end. The chunk over the end is the row's last
-// eight elements shifted down.
-template <typename V> __device__ __forceinline__ Vec8<V> load8(const V* row, int c, int d) {
-  if (c + kVec <= d) return load_full(row + c);
-  Vec8<V> v{};
-  if (c >= d) return v;
-  if (d >= kVec) {
-    v = load_full(row + d - kVec);
-    drop(v, c + kVec - d);
-    return v;
-  }
+// A chunk is the elements c .. c + 7 of a row of d. Where it passes the row's end, load_raw takes
+// the row's last eight elements instead, with no branch around the load, so that the loads of several
+// rows go out together; settle then shifts them to their places, with zeros past the end. (Rows of
+// fewer than eight elements are read one by one and need no settling.)
+template <typename V> __device__ __forceinline__ Vec8<V> load_raw(const V* row, int c, int d) {
+  if (d >= kVec) return load_full(row + min(c, d - kVec));
   V e[kVec] = {};
 #pragma unroll
   for (int i = 0; i < kVec; ++i)
     if (c + i < d) e[i] = row[c + i];
+  Vec8<V> v;
   __builtin_memcpy(&v, e, sizeof(e));
+  return v;
+}
+template <typename V> __device__ __forceinline__ void settle(Vec8<V>& v, int c, int d) {
+  if (c + kVec > d && d >= kVec) drop(v, min(c + kVec - d, kVec));
+}
+template <typename V> __device__ __forceinline__ Vec8<V> load8(const V* row, int c, int d) {
+  Vec8<V> v = load_raw(row, c, d);
+  settle(v, c, d);
   return v;
 }
 
@@ -93,8 +99,8 @@ __device__ __forceinline__ void store_full(float* p, const Vec8<float>& v) {
   store16(p + 4, v.b);
 }
 
-// Eight elements to c .. c + 7 of a row of d; what is past its end is left out (four, two and one
-// elements at a time).
+// Eight elements to a chunk; what is past the row's end is left out (four, two and one elements at
+// a time).
 template <typename V> __device__ __forceinline__ void copy8(V* row, int c, int d, Vec8<V> v) {
   if (c + kVec <= d) return store_full(row + c, v);
   if (c >= d) return;
@@ -113,6 +119,18 @@ template <typename V> __device__ __forceinline__ void copy8(V* row, int c, int d
   if (left & 1) __builtin_memcpy(p, &v, sizeof(V));
 }
 
+// Where a chunk's elements go one by one to the same place of another row, a chunk that load_raw
+// moved back may be stored where it was loaded: its neighbour stores the same values there.
+template <typename V> __device__ __forceinline__ void store_raw(V* row, int c, int d, const Vec8<V>& v) {
+  if (c >= d) return;
+  if (d >= kVec)
+    store_full(row + min(c, d - kVec), v);
+  else
+    copy8(row, c, d, v);
+}
+// Elements of a raw chunk that are its neighbour's.
+__device__ __forceinline__ int raw_overlap(int c, int d) { return d >= kVec ? max(c + kVec - d, 0) : 0; }
+
 // Two floats to packed bf16, each to nearest even (NaN stays a NaN): one v_cvt_pk_bf16_f32.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   typedef float f32x2_t __attribute__((ext_vector_type(2)));
@@ -127,6 +145,9 @@ __device__ __forceinline__ Vec8<bf16_t> rounded(const float (&v)[kVec], bf16_t) 
 }
 __device__ __forceinline__ Vec8<float> rounded(const float (&v)[kVec], float) {
   return {f32x4_t{v[0], v[1], v[2], v[3]}, f32x4_t{v[4], v[5], v[6], v[7]}};
+}
+template <typename V> __device__ __forceinline__ void store8_raw(V* row, int c, int d, const float (&v)[kVec]) {
+  store_raw(row, c, d, rounded(v, V{}));
 }
 template <typename V> __device__ __forceinline__ void store8(V* row, int c, int d, const float (&v)[kVec]) {
   copy8(row, c, d, rounded(v, V{}));
