@@ -18,7 +18,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kListMax = 112;  // ranges of one launch: the list travels as a kernel argument
-constexpr int kTile = kThreads * kVec;  // elements of one step of a workgroup
+constexpr int kTile = 2048;      // smallest share of a workgroup
 
 // Elements of a workgroup's share: all of its loads go out together. Long shares are slower (their
 // last round leaves CUs idle; both passes over 2^27 fp32 elements in two tensors: 304 us with shares
@@ -64,18 +64,45 @@ template <int N> __device__ __forceinline__ double block_sum(double v) {
   return s;
 }
 
-template <typename V> __device__ __forceinline__ double share_sumsq(const V* p, int n) {
-  double s[2] = {0, 0};
-  constexpr int kSteps = kSumShare / kTile;
-  const int c = threadIdx.x * kVec;
-  Vec8<V> v[kSteps];
+// 16 bytes per thread and step, so that every access of a wave is one run of 1 KiB (two times 16
+// bytes per thread side by side: 17 % more bytes written, by the counter, for fp32).
+template <typename V> struct Step {
+  static constexpr int kElems = 16 / sizeof(V), kStep = kThreads * kElems;
+  V e[kElems];
+  __device__ __forceinline__ void load(const V* p, int c, int n) {
+    if (c + kElems <= n) {
+      __builtin_memcpy(e, p + c, 16);
+    } else {
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) v[i] = load8(p, c + i * kTile, n);
+      for (int i = 0; i < kElems; ++i) e[i] = c + i < n ? p[c + i] : V(0);
+    }
+  }
+  __device__ __forceinline__ void store(V* p, int c, int n) const {
+    if (c + kElems <= n) {
+      u32x4_t w;
+      __builtin_memcpy(&w, e, 16);
+      store16(p + c, w);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kElems; ++i)
+        if (c + i < n) p[c + i] = e[i];
+    }
+  }
+};
+
+template <typename V> __device__ __forceinline__ double share_sumsq(const V* p, int n) {
+  using S = Step<V>;
+  constexpr int kSteps = kSumShare / S::kStep;
+  double s[2] = {0, 0};
+  const int c = threadIdx.x * S::kElems;
+  S v[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) v[i].load(p, c + i * S::kStep, n);
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-      const double g = (double)v[i].get(e);
+    for (int e = 0; e < S::kElems; ++e) {
+      const double g = (double)VT<V>::load(v[i].e, e);
       s[e & 1] = fma(g, g, s[e & 1]);
     }
   return s[0] + s[1];
@@ -107,17 +134,17 @@ __global__ __launch_bounds__(kSumThreads) void k_grad_sum(const double* __restri
 
 template <typename V> __device__ __forceinline__ void share_scale(const V* p, V* q, int n, float by) {
   if (p == q && by == 1.f) return;
-  constexpr int kSteps = kScaleShare / kTile;
-  const int c = threadIdx.x * kVec;
-  Vec8<V> v[kSteps];
+  using S = Step<V>;
+  constexpr int kSteps = kScaleShare / S::kStep;
+  const int c = threadIdx.x * S::kElems;
+  S v[kSteps];
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) v[i] = load8(p, c + i * kTile, n);
+  for (int i = 0; i < kSteps; ++i) v[i].load(p, c + i * S::kStep, n);
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    float o[kVec];
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) o[e] = v[i].get(e) * by;
-    store8(q, c + i * kTile, n, o);
+    for (int e = 0; e < S::kElems; ++e) VT<V>::store(v[i].e, e, VT<V>::load(v[i].e, e) * by);
+    v[i].store(q, c + i * S::kStep, n);
   }
 }
 
