@@ -23,8 +23,7 @@ namespace {
 
 // Layout of a launch: rows of up to 512 columns take NT = 8 to 64 threads, R = 256 / NT rows at a
 // time per workgroup; wider ones a workgroup of as many waves as they need, at most NT threads.
-// Every thread has CH chunks of 8 columns, chunk i of thread x at column (i NT + x) 8. It sees the
-// same columns in all of its rows, so it loads their weights once and keeps their parameter sums in
+// Every thread has CH chunks of 8 columns. It sees the same columns in all of its rows, so it loads their weights once and keeps their parameter sums in
 // registers.
 template <int NT> struct Rows {
   static constexpr int kThreads = NT <= kWave ? 256 : NT;
@@ -59,7 +58,7 @@ template <int NT, int n> struct RowSum {
 };
 
 // A parameter's eight values of one chunk; ones where there is no parameter.
-__device__ __forceinline__ void load_param(const float* w, int c, int d, float (&v)[kVec]) {
+__device__ __forceinline__ void load_param(const float* w, Cols c, int d, float (&v)[kVec]) {
   if (!w) {
 #pragma unroll
     for (int i = 0; i < kVec; ++i) v[i] = 1.f;
@@ -71,7 +70,7 @@ __device__ __forceinline__ void load_param(const float* w, int c, int d, float (
 }
 
 // u = w_post gate_c of one chunk.
-template <typename P> __device__ __forceinline__ void load_u(const P& p, int c, int d, float (&u)[kVec]) {
+template <typename P> __device__ __forceinline__ void load_u(const P& p, Cols c, int d, float (&u)[kVec]) {
   float g[kVec];
   load_param(p.w_post, c, d, u);
   load_param(p.gate_c, c, d, g);
@@ -86,11 +85,12 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
   RowSum<NT, 1> row_sum(red);
   const int x = NT <= kWave ? threadIdx.x % NT : threadIdx.x, d = (int)p.d;
   const float inv_d = 1.f / (float)d;
+  const int lanes = NT <= kWave ? NT : blockDim.x;
   float u[CH][kVec], w[CH][kVec];
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
-    load_u(p, (i * NT + x) * kVec, d, u[i]);
-    load_param(p.w_pre, (i * NT + x) * kVec, d, w[i]);
+    load_u(p, cols<V>(i, x, lanes), d, u[i]);
+    load_param(p.w_pre, cols<V>(i, x, lanes), d, w[i]);
   }
   const int64_t step = (int64_t)gridDim.x * L::R;
   // every thread of a workgroup takes as many turns (row_sum has barriers)
@@ -101,13 +101,13 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
     Vec8<V> X[CH], Y[CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const int c = (i * NT + x) * kVec;
+      const Cols c = cols<V>(i, x, lanes);
       X[i] = load_raw((const V*)p.X + base, c, d);
       if (p.Y) Y[i] = load_raw((const V*)p.Y + base, c, d);
     }
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const int c = (i * NT + x) * kVec;
+      const Cols c = cols<V>(i, x, lanes);
       settle(X[i], c, d);
       if (p.Y) settle(Y[i], c, d);
     }
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
       }
     if (p.X_out && in)
 #pragma unroll
-      for (int i = 0; i < CH; ++i) store8((V*)p.X_out + base, (i * NT + x) * kVec, d, o[i]);
+      for (int i = 0; i < CH; ++i) store8((V*)p.X_out + base, cols<V>(i, x, lanes), d, rounded<V>(o[i]));
     if (p.pre) {
       row_sum(s);
       const float rx = rsqrtf(s[0] * inv_d + p.eps);
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
       for (int i = 0; i < CH; ++i) {
 #pragma unroll
         for (int e = 0; e < kVec; ++e) o[i][e] *= rx * w[i][e];
-        if (in) store8((V*)p.N + base, (i * NT + x) * kVec, d, o[i]);
+        if (in) store8((V*)p.N + base, cols<V>(i, x, lanes), d, rounded<V>(o[i]));
       }
     }
   }
@@ -155,14 +155,14 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
 // have twice the bytes in flight without).
 template <typename V> struct BwdRow {
   Vec8<V> X, Y, G, N;  // X_out, Y, dX_out, dN
-  __device__ __forceinline__ void load(const NormBwdParams& p, int64_t base, int c, int d) {
+  __device__ __forceinline__ void load(const NormBwdParams& p, int64_t base, Cols c, int d) {
     X = p.pre ? load_raw((const V*)p.X_out + base, c, d) : Vec8<V>{};
     Y = p.Y ? load_raw((const V*)p.Y + base, c, d) : Vec8<V>{};
     G = p.dX_out ? load_raw((const V*)p.dX_out + base, c, d) : Vec8<V>{};
     N = p.dN ? load_raw((const V*)p.dN + base, c, d) : Vec8<V>{};
   }
-  __device__ __forceinline__ void settled(int c, int d) {
-    if (c + kVec <= d) return;
+  __device__ __forceinline__ void settled(Cols c, int d) {
+    if (raw_whole<V>(c, d)) return;
     settle(X, c, d);
     settle(Y, c, d);
     settle(G, c, d);
@@ -193,52 +193,55 @@ struct BwdCoef {
     gr = gt * ry;
     ky = p.post ? gr * ry * Q * inv_d : 0.f;
   }
-  template <typename V, typename F>
+  // A and S: the chunk's parameter sums, the second four from A[hi] on
+  template <typename V>
   __device__ __forceinline__ void outputs(const NormBwdParams& p, const BwdRow<V>& r, const float (&u)[kVec],
-                                          const float (&w)[kVec], F* A, F* S, int64_t base, int c, int d) const {
+                                          const float (&w)[kVec], float* A, float* S, int hi, int64_t base, Cols c,
+                                          int d) const {
     float dx[kVec], dy[kVec];
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
+      const int at = e < 4 ? e : hi + e - 4;
       const float xv = r.X.get(e), yv = r.Y.get(e), n = r.N.get(e);
       const float D = fmaf(-k, xv, fmaf(rx, n * w[e], r.G.get(e)));
-      A[e] = fmaf(n, xv * rx, A[e]);
-      S[e] = fmaf(D, yv * gr, S[e]);
+      A[at] = fmaf(n, xv * rx, A[at]);
+      S[at] = fmaf(D, yv * gr, S[at]);
       dx[e] = p.res_scale * D;
       dy[e] = fmaf(gr * u[e], D, -ky * yv);
     }
-    if (p.dX) store8((V*)p.dX + base, c, d, dx);
-    if (p.dY) store8((V*)p.dY + base, c, d, dy);
+    if (p.dX) store8((V*)p.dX + base, c, d, rounded<V>(dx));
+    if (p.dY) store8((V*)p.dY + base, c, d, rounded<V>(dy));
   }
 };
 
 template <typename V, int NT, int CH, bool HOLD>
-__global__ __launch_bounds__(Rows<NT>::kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))) void k_norm_bwd(NormBwdParams p) {
+__global__ __launch_bounds__(Rows<NT>::kThreads) 
+    __attribute__((amdgpu_waves_per_eu(sizeof(V) == 2 ? 4 : 3))) void k_norm_bwd(NormBwdParams p) {
   static_assert(!HOLD || CH == 1, "");
   using L = Rows<NT>;
   constexpr bool AHEAD = HOLD && sizeof(V) == 2;
-  extern __shared__ float sums[];  // [R][2][CH * NT * 8]: A, S; with HOLD used at the end where R > 1
+  extern __shared__ float sums[];  // [R][2][CH * NT * 8]: A, S by column; with HOLD used at the end where R > 1
   __shared__ float red[2][RowSum<NT, 6>::kWaves][6];
   RowSum<NT, 6> row_sum(red);
   constexpr int W = CH * NT * kVec;
   const int x = NT <= kWave ? threadIdx.x % NT : threadIdx.x, d = (int)p.d, group = L::R == 1 ? 0 : threadIdx.x / NT;
   const float inv_d = 1.f / (float)d;
-  float* mine = sums + group * 2 * W + x * kVec;  // chunk i at i NT 8, S behind A
+  const int lanes = NT <= kWave ? NT : blockDim.x;
+  float* mine = sums + group * 2 * W;  // S behind A
+  const Cols own = cols<V>(0, x, lanes);
   float u[kVec], w[kVec], A[kVec], S[kVec];
 #pragma unroll
   for (int e = 0; e < kVec; ++e) A[e] = S[e] = 0.f;
   if (HOLD) {
-    load_u(p, x * kVec, d, u);
-    load_param(p.w_pre, x * kVec, d, w);
+    load_u(p, own, d, u);
+    load_param(p.w_pre, own, d, w);
   } else {
-#pragma unroll
-    for (int i = 0; i < CH; ++i)
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) mine[i * NT * kVec + e] = mine[W + i * NT * kVec + e] = 0.f;
+    for (int j = threadIdx.x; j < 2 * W; j += NT) mine[j] = 0.f;  // before the barrier of the first row's sums
   }
   const int64_t step = (int64_t)gridDim.x * L::R;
   auto row_of = [&](int64_t t0) { return L::R == 1 ? t0 : min(t0 + group, p.T - 1); };
   BwdRow<V> now, next;
-  if (AHEAD) next.load(p, row_of((int64_t)blockIdx.x * L::R) * p.d, x * kVec, d);
+  if (AHEAD) next.load(p, row_of((int64_t)blockIdx.x * L::R) * p.d, own, d);
   for (int64_t t0 = (int64_t)blockIdx.x * L::R; t0 < p.T; t0 += step) {
     const int64_t t = row_of(t0), base = t * p.d;
     const bool in = L::R == 1 || t0 + group < p.T;  // a group past the end goes along (barriers) and adds nothing
@@ -247,14 +250,14 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) __attribute__((amdgpu_waves_per
       if (AHEAD)
         now = next;
       else
-        now.load(p, base, x * kVec, d);
-      now.settled(x * kVec, d);
+        now.load(p, base, own, d);
+      now.settled(own, d);
       now.add_to(s, u, w);
-      if (AHEAD && t0 + step < p.T) next.load(p, row_of(t0 + step) * p.d, x * kVec, d);
+      if (AHEAD && t0 + step < p.T) next.load(p, row_of(t0 + step) * p.d, own, d);
     } else {
 #pragma unroll 1
       for (int i = 0; i < CH; ++i) {
-        const int c = (i * NT + x) * kVec;
+        const Cols c = cols<V>(i, x, lanes);
         now.load(p, base, c, d);
         now.settled(c, d);
         load_u(p, c, d, u);
@@ -267,32 +270,33 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) __attribute__((amdgpu_waves_per
     const BwdCoef f(p, s, inv_d, p.gate_t ? p.gate_t[t] : 1.f);
     if (p.dgate_t && x == 0) p.dgate_t[t] = f.Q;
     if (HOLD) {
-      f.outputs(p, now, u, w, A, S, base, x * kVec, d);
+      f.outputs(p, now, u, w, A, S, 4, base, own, d);
     } else {
 #pragma unroll 1
       for (int i = 0; i < CH; ++i) {
-        const int c = (i * NT + x) * kVec;
+        const Cols c = cols<V>(i, x, lanes);
         now.load(p, base, c, d);
         now.settled(c, d);
         load_u(p, c, d, u);
         load_param(p.w_pre, c, d, w);
-        f.outputs(p, now, u, w, mine + i * NT * kVec, mine + W + i * NT * kVec, base, c, d);
+        f.outputs(p, now, u, w, mine + c.c0, mine + W + c.c0, c.c1 - c.c0, base, c, d);
       }
     }
   }
   if (!p.part) return;
   float* part = p.part + (int64_t)blockIdx.x * 2 * d;
   if (HOLD && L::R == 1) {
-    store8(part, x * kVec, d, A);
-    store8(part + d, x * kVec, d, S);
+    store8(part, own, d, rounded<float>(A));
+    store8(part + d, own, d, rounded<float>(S));
     return;
   }
   // the workgroup's R rows at a time, added in row order
   if (HOLD)
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
-      mine[e] = A[e];
-      mine[W + e] = S[e];
+      const int c = e < 4 ? own.c0 + e : own.c1 + e - 4;
+      mine[c] = A[e];
+      mine[W + c] = S[e];
     }
   __syncthreads();
   for (int j = threadIdx.x; j < 2 * W; j += L::kThreads) {
@@ -357,7 +361,7 @@ template <typename F> hipError_t with_layout(int64_t d, F f) {
 
 // Workgroups of the backward. The fewer there are, the more rows each adds up before it leaves its
 // sums, so a CU gets the twelve waves (eight of fp32) that keep the memory busy with full loads, or
-// all sixteen that its registers hold where rows leave lanes idle or are not whole in 16-byte units
+// all sixteen (twelve) that its registers hold where rows leave lanes idle or are not whole in units
 // (rows of 2^26 bytes in all, bf16 d = 4096: 81 us with twelve waves, 89 with sixteen; d = 640: 139
 // and 119; fp32 d = 2048: 81 with eight, 90 with twelve).
 static int64_t bwd_blocks(int64_t T, int64_t d, int bf16) {
@@ -365,7 +369,7 @@ static int64_t bwd_blocks(int64_t T, int64_t d, int bf16) {
   (void)with_layout(d, [&](auto nt, auto, int threads) {
     constexpr int NT = decltype(nt)::value;
     const int64_t chunks = cdiv(d, kVec), lanes = NT <= kWave ? NT : threads;
-    const int waves = d % kVec == 0 && 4 * chunks >= 3 * lanes ? (bf16 ? 12 : 8) : 16;
+    const int waves = d % kVec == 0 && 4 * chunks >= 3 * lanes ? (bf16 ? 12 : 8) : (bf16 ? 16 : 12);
     blocks = std::min<int64_t>(cdiv(T, Rows<NT>::R), 256 * std::max(1, waves * kWave / threads));
     return hipSuccess;
   });

@@ -89,15 +89,14 @@ __global__ __launch_bounds__(kThreads) void k_expert_small(const int32_t* __rest
     for (int e = threadIdx.x; e < E; e += kThreads) offsets[e] = cnt[e];
     return;
   }
-  constexpr int W = kThreads / kWave, kStep = kThreads * kVec;
+  constexpr int W = kThreads / kWave;
   const int wave = threadIdx.x / kWave;
   // the row's first chunks come in while the slots are counted
   const V* from = X + t * d;
-  const int c0 = threadIdx.x * kVec;
   Vec8<V> v[2];
   if (X)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) v[i] = load_raw(from, c0 + i * kStep, (int)d);
+    for (int i = 0; i < 2; ++i) v[i] = load_raw(from, cols<V>(i, threadIdx.x, kThreads), (int)d);
   int mine[kSmallPer];
 #pragma unroll
   for (int i = 0; i < kSmallPer; ++i) {
@@ -127,15 +126,15 @@ __global__ __launch_bounds__(kThreads) void k_expert_small(const int32_t* __rest
   }
   if (!X) return;
   __syncthreads();
-  for (int64_t c = c0; c < d; c += 2 * kStep) {
-    if (c != c0)
+  for (int i0 = 0; cols<V>(i0, threadIdx.x, kThreads).c0 < d; i0 += 2) {
+    if (i0)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) v[i] = load_raw(from, (int)c + i * kStep, (int)d);
+      for (int i = 0; i < 2; ++i) v[i] = load_raw(from, cols<V>(i0 + i, threadIdx.x, kThreads), (int)d);
     for (int j = 0; j < k; ++j) {
       const int p = cnt[kRouteMaxK * W + j];
       if (p >= 0 && p < rows)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) store_raw(Xs + p * d, (int)c + i * kStep, (int)d, v[i]);
+        for (int i = 0; i < 2; ++i) store_raw(Xs + p * d, cols<V>(i0 + i, threadIdx.x, kThreads), (int)d, v[i]);
     }
   }
 }
@@ -239,15 +238,16 @@ __global__ __launch_bounds__(kThreads) void k_expert_rows(const V* __restrict__ 
   if (t >= T) return;
   const int d = (int)d64;
   const V* from = X + t * d64;
-  for (int c = threadIdx.x % NT * kVec; c < d; c += kRowChunks * NT * kVec) {
+  const int x = threadIdx.x % NT;
+  for (int i0 = 0; cols<V>(i0, x, NT).c0 < d; i0 += kRowChunks) {
     Vec8<V> v[kRowChunks];
 #pragma unroll
-    for (int i = 0; i < kRowChunks; ++i) v[i] = load_raw(from, c + i * NT * kVec, d);
+    for (int i = 0; i < kRowChunks; ++i) v[i] = load_raw(from, cols<V>(i0 + i, x, NT), d);
     for (int j = 0; j < k; ++j) {
       const int p = pos[t * k + j];
       if (p >= 0 && p < rows)
 #pragma unroll
-        for (int i = 0; i < kRowChunks; ++i) store_raw(Xs + p * d64, c + i * NT * kVec, d, v[i]);
+        for (int i = 0; i < kRowChunks; ++i) store_raw(Xs + p * d64, cols<V>(i0 + i, x, NT), d, v[i]);
     }
   }
 }
@@ -262,7 +262,9 @@ __global__ __launch_bounds__(kThreads) void k_expert_combine(const V* __restrict
   const int64_t t = (int64_t)blockIdx.x * (kThreads / NT) + threadIdx.x / NT;
   if (t >= T) return;
   const int d = (int)d64;
-  for (int c = threadIdx.x % NT * kVec; c < d; c += NT * kVec) {
+  for (int i = 0;; ++i) {
+    const Cols c = cols<V>(i, threadIdx.x % NT, NT);
+    if (c.c0 >= d) break;
     float s[kVec] = {};
     for (int j0 = 0; j0 < k; j0 += KS) {
       Vec8<V> v[KS];
@@ -282,7 +284,7 @@ __global__ __launch_bounds__(kThreads) void k_expert_combine(const V* __restrict
 #pragma unroll
           for (int e = 0; e < kVec; ++e) s[e] = fmaf(w[j], v[j].get(e), s[e]);
     }
-    store8_raw(Y + t * d64, c, d, s);
+    store_raw(Y + t * d64, c, d, rounded<V>(s));
   }
 }
 
@@ -311,9 +313,11 @@ __global__ __launch_bounds__(kThreads) void k_expert_combine_bwd(const V* __rest
       w[j] = weight ? weight[slot] : 1.f;
       dot[j] = 0.f;
     }
-    for (int c = threadIdx.x % NT * kVec; c < d; c += NT * kVec) {
+    for (int i = 0;; ++i) {
+      const Cols c = cols<V>(i, threadIdx.x % NT, NT);
+      if (c.c0 >= d) break;
       const Vec8<V> g = load_raw(dY + t * d64, c, d);
-      const int skip = raw_overlap(c, d);  // these count in the neighbour's dot product
+      const bool whole = raw_whole<V>(c, d);  // else some elements count in the neighbour's dot product
       Vec8<V> v[KS];
       if (dweight)
 #pragma unroll
@@ -323,19 +327,19 @@ __global__ __launch_bounds__(kThreads) void k_expert_combine_bwd(const V* __rest
       for (int j = 0; j < KS; ++j) {
         if (p[j] < 0) continue;
         if (dweight) {
-          if (skip == 0) {
+          if (whole) {
 #pragma unroll
             for (int e = 0; e < kVec; ++e) dot[j] = fmaf(g.get(e), v[j].get(e), dot[j]);
           } else {
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) dot[j] = e < skip ? dot[j] : fmaf(g.get(e), v[j].get(e), dot[j]);
+            for (int e = 0; e < kVec; ++e) dot[j] = raw_own<V>(e, c, d) ? fmaf(g.get(e), v[j].get(e), dot[j]) : dot[j];
           }
         }
         if (dYs) {
           float o[kVec];
 #pragma unroll
           for (int e = 0; e < kVec; ++e) o[e] = w[j] * g.get(e);
-          store8_raw(dYs + p[j] * d64, c, d, o);
+          store_raw(dYs + p[j] * d64, c, d, rounded<V>(o));
         }
       }
     }

@@ -1,14 +1,31 @@
-// Row access shared by the operators around the layer: eight consecutive elements of a row per
-// thread, whatever the row's alignment, and sums over the threads of a row.
+// Row access shared by the operators around the layer: eight elements of a row per thread, whatever
+// the row's alignment, and sums over the threads of a row.
 #pragma once
 
 #include "common.h"
 
 namespace sfl {
 
-constexpr int kVec = 8;  // elements of one load: 16 bytes of bf16, two times 16 of fp32
+constexpr int kVec = 8;  // elements of a chunk
 
-// Eight elements as loaded (bf16 stays packed until it is used).
+// A chunk: the eight columns that a thread has of a row, in 16-byte units, so that every access of a
+// wave is one run of 1 KiB: eight columns from c0 in bf16, four from c0 and four from c1 in fp32. (Two
+// fp32 units side by side wrote 29 % more bytes than there are, by the counter: the wave's stores
+// reach a cache line in two halves.)
+struct Cols {
+  int c0, c1;
+};
+// Chunk i of thread x of the L threads of a row.
+template <typename V> __device__ __forceinline__ Cols cols(int i, int x, int L) {
+  if (sizeof(V) == 2) {
+    const int c = (i * L + x) * kVec;
+    return {c, c + 4};
+  }
+  const int c = i * L * kVec + x * 4;
+  return {c, c + L * 4};
+}
+
+// A chunk's elements as loaded (bf16 stays packed until it is used).
 template <typename V> struct Vec8;
 template <> struct Vec8<bf16_t> {
   u32x4_t w;
@@ -36,12 +53,9 @@ template <typename T, typename P> __device__ __forceinline__ void store16(P* p, 
   __builtin_nontemporal_store(w, (u32x4_any_t*)p);
 }
 
-__device__ __forceinline__ Vec8<bf16_t> load_full(const bf16_t* p) { return {load16<u32x4_t>(p)}; }
-__device__ __forceinline__ Vec8<float> load_full(const float* p) { return {load16<f32x4_t>(p), load16<f32x4_t>(p + 4)}; }
-
-// Drops the first s <= 8 of eight elements and lets zeros in behind them.
-__device__ __forceinline__ void drop(Vec8<bf16_t>& v, int s) {
-  uint64_t lo = (uint64_t)v.w[1] << 32 | v.w[0], hi = (uint64_t)v.w[3] << 32 | v.w[2];
+// Drops the first s elements (at most all) of a unit and lets zeros in behind them.
+__device__ __forceinline__ void drop(u32x4_t& w, int s) {
+  uint64_t lo = (uint64_t)w[1] << 32 | w[0], hi = (uint64_t)w[3] << 32 | w[2];
   if (s & 4) {
     lo = hi;
     hi = 0;
@@ -52,84 +66,94 @@ __device__ __forceinline__ void drop(Vec8<bf16_t>& v, int s) {
     hi >>= bits;
   }
   if (s & 8) lo = hi = 0;
-  v.w = u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+  w = u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
-__device__ __forceinline__ void drop(Vec8<float>& v, int s) {
-  if (s & 4) {
-    v.a = v.b;
-    v.b = f32x4_t{};
-  }
-  if (s & 2) {
-    v.a = f32x4_t{v.a[2], v.a[3], v.b[0], v.b[1]};
-    v.b = f32x4_t{v.b[2], v.b[3], 0.f, 0.f};
-  }
-  if (s & 1) {
-    v.a = f32x4_t{v.a[1], v.a[2], v.a[3], v.b[0]};
-    v.b = f32x4_t{v.b[1], v.b[2], v.b[3], 0.f};
-  }
-  if (s & 8) v.a = v.b = f32x4_t{};
+__device__ __forceinline__ void drop(f32x4_t& v, int s) {
+  if (s & 2) v = f32x4_t{v[2], v[3], 0.f, 0.f};
+  if (s & 1) v = f32x4_t{v[1], v[2], v[3], 0.f};
+  if (s & 4) v = f32x4_t{};
 }
 
-// A chunk is the elements c .. c + 7 of a row of d. Where it passes the row's end, load_raw takes
-// the row's last eight elements instead, with no branch around the load, so that the loads of several
-// rows go out together; settle then shifts them to their places, with zeros past the end. (Rows of
-// fewer than eight elements are read one by one and need no settling.)
-template <typename V> __device__ __forceinline__ Vec8<V> load_raw(const V* row, int c, int d) {
-  if (d >= kVec) return load_full(row + min(c, d - kVec));
-  V e[kVec] = {};
+// Units of N elements of type V, held as U. Where a unit passes the row's end, load_unit takes the
+// row's last N elements instead, with no branch around the load, so that the loads of several rows
+// go out together; settle_unit then shifts them to their places, with zeros past the end. (Rows of
+// fewer than N elements are read one by one and need no settling.)
+template <typename U, typename V> __device__ __forceinline__ U load_unit(const V* row, int c, int d) {
+  constexpr int N = 16 / sizeof(V);
+  if (d >= N) return load16<U>(row + min(c, d - N));
+  V e[N] = {};
 #pragma unroll
-  for (int i = 0; i < kVec; ++i)
+  for (int i = 0; i < N; ++i)
     if (c + i < d) e[i] = row[c + i];
-  Vec8<V> v;
-  __builtin_memcpy(&v, e, sizeof(e));
+  U v;
+  __builtin_memcpy(&v, e, 16);
   return v;
 }
-template <typename V> __device__ __forceinline__ void settle(Vec8<V>& v, int c, int d) {
-  if (c + kVec > d && d >= kVec) drop(v, min(c + kVec - d, kVec));
+template <int N, typename U> __device__ __forceinline__ void settle_unit(U& v, int c, int d) {
+  if (c + N > d && d >= N) drop(v, min(c + N - d, N));
 }
-template <typename V> __device__ __forceinline__ Vec8<V> load8(const V* row, int c, int d) {
+// What is past the row's end is left out (N / 2, ... and one element at a time).
+template <typename U, typename V> __device__ __forceinline__ void store_unit(V* row, int c, int d, U v) {
+  constexpr int N = 16 / sizeof(V);
+  if (c + N <= d) return store16(row + c, v);
+  if (c >= d) return;
+  V* p = row + c;
+#pragma unroll
+  for (int n = N / 2; n > 0; n /= 2)
+    if ((d - c) & n) {
+      __builtin_memcpy(p, &v, n * sizeof(V));
+      p += n;
+      drop(v, n);
+    }
+}
+// Where a unit's elements go one by one to the same place of another row, a unit that load_unit moved
+// back may be stored where it was loaded: its neighbour stores the same values there.
+template <typename U, typename V> __device__ __forceinline__ void store_unit_raw(V* row, int c, int d, const U& v) {
+  constexpr int N = 16 / sizeof(V);
+  if (c >= d) return;
+  if (d >= N)
+    store16(row + min(c, d - N), v);
+  else
+    store_unit(row, c, d, v);
+}
+
+// The same for chunks.
+__device__ __forceinline__ Vec8<bf16_t> load_raw(const bf16_t* row, Cols c, int d) { return {load_unit<u32x4_t>(row, c.c0, d)}; }
+__device__ __forceinline__ Vec8<float> load_raw(const float* row, Cols c, int d) {
+  return {load_unit<f32x4_t>(row, c.c0, d), load_unit<f32x4_t>(row, c.c1, d)};
+}
+__device__ __forceinline__ void settle(Vec8<bf16_t>& v, Cols c, int d) { settle_unit<8>(v.w, c.c0, d); }
+__device__ __forceinline__ void settle(Vec8<float>& v, Cols c, int d) {
+  settle_unit<4>(v.a, c.c0, d);
+  settle_unit<4>(v.b, c.c1, d);
+}
+template <typename V> __device__ __forceinline__ Vec8<V> load8(const V* row, Cols c, int d) {
   Vec8<V> v = load_raw(row, c, d);
   settle(v, c, d);
   return v;
 }
-
-__device__ __forceinline__ void store_full(bf16_t* p, const Vec8<bf16_t>& v) { store16(p, v.w); }
-__device__ __forceinline__ void store_full(float* p, const Vec8<float>& v) {
-  store16(p, v.a);
-  store16(p + 4, v.b);
+__device__ __forceinline__ void store8(bf16_t* row, Cols c, int d, const Vec8<bf16_t>& v) { store_unit(row, c.c0, d, v.w); }
+__device__ __forceinline__ void store8(float* row, Cols c, int d, const Vec8<float>& v) {
+  store_unit(row, c.c0, d, v.a);
+  store_unit(row, c.c1, d, v.b);
 }
-
-// Eight elements to a chunk; what is past the row's end is left out (four, two and one elements at
-// a time).
-template <typename V> __device__ __forceinline__ void copy8(V* row, int c, int d, Vec8<V> v) {
-  if (c + kVec <= d) return store_full(row + c, v);
-  if (c >= d) return;
-  V* p = row + c;
-  const int left = d - c;
-  if (left & 4) {
-    __builtin_memcpy(p, &v, 4 * sizeof(V));
-    p += 4;
-    drop(v, 4);
-  }
-  if (left & 2) {
-    __builtin_memcpy(p, &v, 2 * sizeof(V));
-    p += 2;
-    drop(v, 2);
-  }
-  if (left & 1) __builtin_memcpy(p, &v, sizeof(V));
+__device__ __forceinline__ void store_raw(bf16_t* row, Cols c, int d, const Vec8<bf16_t>& v) {
+  store_unit_raw(row, c.c0, d, v.w);
 }
-
-// Where a chunk's elements go one by one to the same place of another row, a chunk that load_raw
-// moved back may be stored where it was loaded: its neighbour stores the same values there.
-template <typename V> __device__ __forceinline__ void store_raw(V* row, int c, int d, const Vec8<V>& v) {
-  if (c >= d) return;
-  if (d >= kVec)
-    store_full(row + min(c, d - kVec), v);
-  else
-    copy8(row, c, d, v);
+__device__ __forceinline__ void store_raw(float* row, Cols c, int d, const Vec8<float>& v) {
+  store_unit_raw(row, c.c0, d, v.a);
+  store_unit_raw(row, c.c1, d, v.b);
 }
-// Elements of a raw chunk that are its neighbour's.
-__device__ __forceinline__ int raw_overlap(int c, int d) { return d >= kVec ? max(c + kVec - d, 0) : 0; }
+// Whether element e of a raw chunk is there and not its neighbour's (all are where every unit is
+// whole: ask raw_whole first).
+template <typename V> __device__ __forceinline__ bool raw_whole(Cols c, int d) {
+  return (sizeof(V) == 2 ? c.c0 + 8 : c.c1 + 4) <= d;
+}
+template <typename V> __device__ __forceinline__ bool raw_own(int e, Cols c, int d) {
+  constexpr int N = 16 / sizeof(V);
+  const int at = e < N ? c.c0 : c.c1;
+  return d < N || e % N >= at + N - d;
+}
 
 // Two floats to packed bf16, each to nearest even (NaN stays a NaN): one v_cvt_pk_bf16_f32.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -139,18 +163,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   __builtin_memcpy(&w, &v, 4);
   return w;
 }
-
-__device__ __forceinline__ Vec8<bf16_t> rounded(const float (&v)[kVec], bf16_t) {
+template <typename V> __device__ __forceinline__ Vec8<V> rounded(const float (&v)[kVec]);
+template <> __device__ __forceinline__ Vec8<bf16_t> rounded<bf16_t>(const float (&v)[kVec]) {
   return {u32x4_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])}};
 }
-__device__ __forceinline__ Vec8<float> rounded(const float (&v)[kVec], float) {
+template <> __device__ __forceinline__ Vec8<float> rounded<float>(const float (&v)[kVec]) {
   return {f32x4_t{v[0], v[1], v[2], v[3]}, f32x4_t{v[4], v[5], v[6], v[7]}};
-}
-template <typename V> __device__ __forceinline__ void store8_raw(V* row, int c, int d, const float (&v)[kVec]) {
-  store_raw(row, c, d, rounded(v, V{}));
-}
-template <typename V> __device__ __forceinline__ void store8(V* row, int c, int d, const float (&v)[kVec]) {
-  copy8(row, c, d, rounded(v, V{}));
 }
 
 template <int CTRL> __device__ __forceinline__ float dpp_add(float v) {
