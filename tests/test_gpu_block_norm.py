@@ -113,6 +113,35 @@ def test_element_alignment(d, dt):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("widths", [range(1, 20), (31, 33, 63, 65, 127, 129, 255, 511, 513, 519), (1023, 1025, 2047, 2049),
+                                    (4095, 4097, 8191, 8193)], ids=lambda w: f"{min(w)}-{max(w)}")
+def test_widths_around_the_kernels_units(widths, dt):
+    """Rows that end anywhere in a thread's, a wave's or a workgroup's columns."""
+    for d in widths:
+        forward(3, d, dt, FORMS[0], seed=d)
+        backward(3, d, dt, FORMS[0], seed=d)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [61, 1003, 8197])
+def test_in_place_at_odd_widths(d, dt):
+    T = 40
+    dev, _, norms = setup(T, d, dt, FORMS[2], 7)
+    kw = dict(norms=norms, res_scale=0.5, w_pre=dev["w_pre"])
+    X1, N1, X2, N2 = (torch.empty_like(dev["X"]) for _ in range(4))
+    X2.copy_(dev["X"])
+    b.sfl_norm_forward(dev["X"], dev["Y"], X_out=X1, N=N1, **kw)
+    b.sfl_norm_forward(X2, dev["Y"], X_out=X2, N=N2, **kw)
+    assert same_bits(X1, X2) and same_bits(N1, N2)
+    ws = torch.empty(b.sfl_norm_workspace_size(T, d, dt), dtype=torch.uint8, device="cuda")
+    dX1, dX2, dY1, dY2 = (torch.empty_like(X1) for _ in range(4))
+    dX2.copy_(dev["dX_out"])
+    b.sfl_norm_backward(X1, dev["Y"], dev["dX_out"], dev["dN"], dX=dX1, dY=dY1, workspace=ws, **kw)
+    b.sfl_norm_backward(X1, dev["Y"], dX2, dev["dN"], dX=dX2, dY=dY2, workspace=ws, **kw)
+    assert same_bits(dX1, dX2) and same_bits(dY1, dY2)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_in_place_and_unwanted_outputs(dt):
     T, d = 19, 520
     dev, _, norms = setup(T, d, dt, FORMS[0], 3)

@@ -107,6 +107,16 @@ def test_element_alignment(dt):
             test_rows_there_and_back(40, d, 2, 6, "holes", dt, by)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("widths", [range(1, 20), (63, 65, 127, 129, 255, 511, 513, 1023, 1025, 2047, 2049, 4097)],
+                         ids=lambda w: f"{min(w)}-{max(w)}")
+def test_widths_around_the_kernels_units(widths, dt):
+    """Rows that end anywhere in a thread's or a workgroup's columns; one and several launches."""
+    for d in widths:
+        test_rows_there_and_back(9, d, 3, 4, "holes", dt)
+        test_rows_there_and_back(1100 if d < 600 else 5, d, 2, 4, "holes", dt)
+
+
 def test_fewer_rows_than_slots_and_foreign_positions():
     """Rows beyond the buffer are not written; positions outside it add nothing."""
     T, k, E, d, rows = 50, 2, 4, 72, 60

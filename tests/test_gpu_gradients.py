@@ -62,6 +62,37 @@ def test_clip(sizes, kinds, in_place):
     check(sizes, kinds, 0.0, by=3, in_place=in_place)
 
 
+def test_views_of_one_bucket():
+    """Tensors that lie end to end go as one range: with gaps, other types and empty tensors among
+    them, in order and not, in place and to buckets laid out alike and otherwise."""
+    r = np.random.default_rng(3)
+    flat = {"f32": torch.empty(40000, device="cuda"), "bf16": torch.empty(40000, device="cuda", dtype=torch.bfloat16)}
+    vals = {n: stored(r.standard_normal(40000), n) for n in flat}
+    for lens, order, skip in [([5000] * 8, range(8), 0), ([1, 4095, 4097, 0, 3, 20000, 7], range(7), 0),
+                              ([5000] * 8, [3, 4, 5, 0, 1, 7, 6, 2], 0), ([999] * 20, range(20), 1)]:
+        for n in flat:
+            flat[n].copy_(vals[n][0])
+        at = np.concatenate([[0], np.cumsum([l + skip for l in lens])])
+        src = [flat["bf16" if i % 3 == 2 else "f32"][at[i]:at[i] + lens[i]] for i in order]
+        want = torch.cat([t.double() for t in src])
+        out = torch.empty(2 * sum(lens) + 64, device="cuda")
+        halves = torch.empty(2 * sum(lens) + 64, device="cuda", dtype=torch.bfloat16)
+        dst, a = [], 0
+        for i, t in zip(order, src):
+            dst.append((out if t.dtype == torch.float32 else halves)[a:a + t.numel()])
+            a += t.numel() + (16 if i % 2 else 0)
+        norm = torch.empty(1, device="cuda")
+        q = total(b.grad_list(src))
+        assert abs(q.item() - want.square().sum().item()) <= 1e-12 * q.item()
+        b.sfl_grad_clip(b.grad_list(src, dst), q, 1.0, norm)
+        b.sfl_grad_clip(b.grad_list(src), q, 1.0)
+        by = 1.0 / math.sqrt(q.item())
+        for got in (dst, src):
+            for g, w in zip(got, want.split([t.numel() for t in src])):
+                w = (w * by).cpu().numpy()
+                assert_rounded(g.cpu().double().numpy(), w, np.abs(w), "f32" if g.dtype == torch.float32 else "bf16", 4)
+
+
 @pytest.mark.parametrize("std", [1e-30, 1e-22, 1e18, 1e30])
 def test_squares_outside_the_fp32_range(std):
     check([5000, 333], ["f32", "bf16"], std, std=std)
