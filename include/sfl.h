@@ -457,8 +457,8 @@ sfl_status_t sfl_down_projection_rowwise(const sfl_ffn_args_t* args, int32_t spl
  * when it trains it. The conventions above hold: caller-owned contiguous row-major buffers, no
  * allocation, no synchronisation, errors before any launch. Rows are bf16 or fp32 (dtype);
  * parameters, gates, weights and their gradients are fp32; sums are held in fp32 (the gradient
- * norm in fp64) in a fixed order, so results are the same from call to call. Pointers need the
- * alignment of their element type only; a row of any width is served. */
+ * norm in fp64) in a fixed order, so a call repeated on the same buffers gives the same bits.
+ * Pointers need the alignment of their element type only; a row of any width is served. */
 
 /* Which norms a block's boundary has. */
 enum {
@@ -470,7 +470,8 @@ enum {
  *   P = Y r_y w_post, r_y = 1 / sqrt(mean(Y[t]^2) + eps)   (SFL_NORM_POST; else P = Y)
  *   X_out = res_scale X + gate_t[t] gate_c P
  *   N = X_out r_x w_pre, r_x = 1 / sqrt(mean(X_out[t]^2) + eps)   (SFL_NORM_PRE)
- * N is formed from X_out before its rounding to dtype.
+ * N is formed from X_out before its rounding to dtype. Squares are formed in fp32: a row with a
+ * magnitude above 1.8e19 has an infinite mean square, and a norm of zeros.
  *  norms   SFL_NORM_* bits
  *  T, d    rows and width, d <= 16384
  *  eps     added to the mean square, >= 0
@@ -504,7 +505,8 @@ typedef struct {
  *  dY      [T][d] gradient of Y, overlaps no input, or NULL
  *  dw_pre, dw_post, dgate_c [d], dgate_t [T]   fp32, overwritten, each NULL where it is not
  *          wanted (a gradient of a weight that was NULL is that of a weight of ones)
- *  workspace   sfl_norm_workspace_size() bytes, 4-byte aligned */
+ *  workspace   sfl_norm_workspace_size() bytes, 4-byte aligned (also where no parameter's gradient
+ *          is wanted) */
 typedef struct {
   sfl_dtype_t dtype;
   int32_t norms;
@@ -535,7 +537,7 @@ typedef struct {
 sfl_status_t sfl_norm_forward(const sfl_norm_args_t* args, sfl_stream_t stream);
 sfl_status_t sfl_norm_backward(const sfl_norm_bwd_args_t* args, sfl_stream_t stream);
 
-/* Workspace bytes of sfl_norm_backward. */
+/* Workspace bytes of sfl_norm_backward for rows of dtype. */
 sfl_status_t sfl_norm_workspace_size(int64_t T, int64_t d, sfl_dtype_t dtype, size_t* bytes);
 
 /* Router: the k largest logits of each token and their softmax weights.

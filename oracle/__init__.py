@@ -23,6 +23,9 @@ Language Models"):
 * `training` - the dead-unit record (a unit is dead for a training step when it
              was never active in it) and the targeted re-initialisation of dead
              units' gate-projection columns (appendix on training modifications).
+* `block`  - the operators around the layer: block norms with gates and residual sum,
+             the top-k router, tokens into expert order and back, clipping by the
+             global norm, each with its gradient.
 
 Everything is computed in float64 on the *stored* inputs (bf16 bit patterns
 or float32 values widened exactly). Pins: every function is checked by the
