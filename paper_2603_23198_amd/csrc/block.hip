@@ -23,8 +23,8 @@ namespace {
 
 // Layout of a launch: rows of up to 512 columns take NT = 8 to 64 threads, R = 256 / NT rows at a
 // time per workgroup; wider ones a workgroup of as many waves as they need, at most NT threads.
-// Every thread has CH chunks of 8 columns. It sees the same columns in all of its rows, so it loads their weights once and keeps their parameter sums in
-// registers.
+// Every thread has CH chunks of 8 columns. It sees the same columns in all of its rows, so it loads
+// their weights once and keeps their parameter sums in registers.
 template <int NT> struct Rows {
   static constexpr int kThreads = NT <= kWave ? 256 : NT;
   static constexpr int R = kThreads / NT;
@@ -184,14 +184,14 @@ template <typename V> struct BwdRow {
 
 // What the outputs of a row take from its sums.
 struct BwdCoef {
-  float rx, k, gr, ky, Q;  // D = dX' + rx g - k x, dY = gr u D - ky y
+  float rx, k, gr, my, Q;  // D = dX' + rx g - k x, dY = gr u D - my (gr y)
   __device__ __forceinline__ BwdCoef(const NormBwdParams& p, const float (&s)[6], float inv_d, float gt) {
     rx = p.pre ? rsqrtf(s[0] * inv_d + p.eps) : 0.f;
-    k = rx * rx * rx * (s[1] * inv_d);
+    k = rx * (rx * (rx * (s[1] * inv_d)));  // in this order: rx^3 alone overflows for rows of about 1e-13
     const float ry = p.post ? rsqrtf(s[2] * inv_d + p.eps) : 1.f;
     Q = ry * (s[3] + rx * s[4] - k * s[5]);
     gr = gt * ry;
-    ky = p.post ? gr * ry * Q * inv_d : 0.f;
+    my = p.post ? ry * (Q * inv_d) : 0.f;
   }
   // A and S: the chunk's parameter sums, the second four from A[hi] on
   template <typename V>
@@ -202,12 +202,12 @@ struct BwdCoef {
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
       const int at = e < 4 ? e : hi + e - 4;
-      const float xv = r.X.get(e), yv = r.Y.get(e), n = r.N.get(e);
+      const float xv = r.X.get(e), yg = r.Y.get(e) * gr, n = r.N.get(e);
       const float D = fmaf(-k, xv, fmaf(rx, n * w[e], r.G.get(e)));
       A[at] = fmaf(n, xv * rx, A[at]);
-      S[at] = fmaf(D, yv * gr, S[at]);
+      S[at] = fmaf(D, yg, S[at]);
       dx[e] = p.res_scale * D;
-      dy[e] = fmaf(gr * u[e], D, -ky * yv);
+      dy[e] = fmaf(gr * u[e], D, -my * yg);
     }
     if (p.dX) store8((V*)p.dX + base, c, d, rounded<V>(dx));
     if (p.dY) store8((V*)p.dY + base, c, d, rounded<V>(dy));
@@ -215,7 +215,7 @@ struct BwdCoef {
 };
 
 template <typename V, int NT, int CH, bool HOLD>
-__global__ __launch_bounds__(Rows<NT>::kThreads) 
+__global__ __launch_bounds__(Rows<NT>::kThreads)
     __attribute__((amdgpu_waves_per_eu(sizeof(V) == 2 ? 4 : 3))) void k_norm_bwd(NormBwdParams p) {
   static_assert(!HOLD || CH == 1, "");
   using L = Rows<NT>;
@@ -313,10 +313,10 @@ __global__ __launch_bounds__(Rows<NT>::kThreads)
 constexpr int kSumCols = 32, kSumThreads = 1024;
 __global__ __launch_bounds__(kSumThreads) void k_norm_param_sums(NormBwdParams p, int blocks) {
   __shared__ float red[kSumThreads / kSumCols][kSumCols];
-  const int64_t cols = cdiv(p.d, kSumCols);
-  const bool second = blockIdx.x >= cols;
+  const int64_t groups = cdiv(p.d, kSumCols);
+  const bool second = blockIdx.x >= groups;
   if (second ? !p.dw_post && !p.dgate_c : !p.dw_pre) return;
-  const int64_t c = (int64_t)(blockIdx.x - (second ? cols : 0)) * kSumCols + threadIdx.x % kSumCols;
+  const int64_t c = (int64_t)(blockIdx.x - (second ? groups : 0)) * kSumCols + threadIdx.x % kSumCols;
   const int g = threadIdx.x / kSumCols;
   float v = 0.f;
   if (c < p.d) {

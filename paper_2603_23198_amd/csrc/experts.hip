@@ -7,7 +7,7 @@
 // The passes over the rows are bound by memory and walk the tokens, so a token's own row is read
 // or written once however many experts it has; the expert side's rows (1 + k or 1 + 2 k rows of
 // traffic per token in all) are whole contiguous rows wherever they lie. Sums run over j in order,
-// in fp32, and no sum depends on another token: there are no atomics.
+// in fp32, and no sum depends on another token; only whole-number counts are atomic.
 #include "block.h"
 #include "rows.h"
 

@@ -151,8 +151,9 @@ template <typename V> __device__ __forceinline__ void share_scale(const V* p, V*
 __global__ __launch_bounds__(kThreads) void k_grad_scale(GradList l, const double* __restrict__ sumsq, float max_norm,
                                                          float* __restrict__ norm) {
   const double nrm = sqrt(*sumsq);
-  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)nrm;
-  const float by = nrm > (double)max_norm && nrm < (double)INFINITY ? (float)((double)max_norm / nrm) : 1.f;
+  const float shown = (float)nrm;  // infinite where fp32 cannot hold it, and then nothing is scaled
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = shown;
+  const float by = nrm > (double)max_norm && shown < INFINITY ? (float)((double)max_norm / nrm) : 1.f;
   if (l.count == 0) return;
   const int b = gridDim.x - 1 - blockIdx.x, i = range_of(l, b);
   const int64_t at = (int64_t)(b - l.first[i]) * l.share;

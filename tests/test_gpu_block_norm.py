@@ -122,6 +122,31 @@ def test_widths_around_the_kernels_units(widths, dt):
         backward(3, d, dt, FORMS[0], seed=d)
 
 
+@pytest.mark.parametrize("scale", [1e-15, 1e-13, 1e13, 1e15])
+def test_magnitudes_far_from_one(scale):
+    """Rows whose squares are still normal fp32 numbers (and their sums finite) keep their accuracy,
+    eps or none."""
+    T, d = 5, 300
+    dev, val, norms = setup(T, d, "f32", FORMS[0], 23)
+    for n in ("X", "Y"):
+        dev[n], val[n] = stored(scale * val[n], "f32")
+    kw = dict(res_scale=0.75, eps=0.0)
+    out = {n: torch.empty_like(dev["X"]) for n in ("X_out", "N")}
+    b.sfl_norm_forward(dev["X"], dev["Y"], norms=norms, **out, **kw, **{n: dev[n] for n in PARAMS})
+    want = block.norm_forward(val["X"], val["Y"], pre=True, post=True, **kw, **{n: val[n] for n in PARAMS})
+    for n, w in zip(("X_out", "N"), want):
+        assert_rounded(out[n].cpu().double().numpy(), *w, "f32", d / 64 + 64, n)
+    ws = torch.empty(b.sfl_norm_workspace_size(T, d, "f32"), dtype=torch.uint8, device="cuda")
+    g = {n: torch.empty_like(dev["X"]) for n in ("dX", "dY")}
+    g.update({"d" + n: torch.empty_like(dev[n]) for n in PARAMS})
+    b.sfl_norm_backward(dev["X"], dev["Y"], dev["dX_out"], dev["dN"], norms=norms, workspace=ws, **g, **kw,
+                        **{n: dev[n] for n in PARAMS})
+    want = block.norm_backward(val["X"], val["Y"], val["dX_out"], val["dN"], pre=True, post=True, **kw,
+                               **{n: val[n] for n in PARAMS})
+    for n, t in g.items():
+        assert_rounded(t.cpu().double().numpy(), *want[n], "f32", d / 64 + 64 + T, n)
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [61, 1003, 8197])
 def test_in_place_at_odd_widths(d, dt):

@@ -121,6 +121,14 @@ def test_a_norm_that_is_not_finite_scales_nothing(bad, in_place):
         assert same_bits(out[0], a0) and same_bits(out[1], c0)
 
 
+def test_a_norm_that_fp32_cannot_hold_is_infinite():
+    a = torch.full((10000,), 3e37, device="cuda")  # norm 3e39
+    grads = b.grad_list([a])
+    q, norm = total(grads), torch.zeros(1, device="cuda")
+    b.sfl_grad_clip(grads, q, 1.0, norm)
+    assert math.isinf(norm.item()) and (a == 3e37).all() and abs(q.item() / (1e4 * a[0].item() ** 2) - 1) < 1e-12
+
+
 def test_ranks_add_their_sums():
     """Two shards of one list, clipped by the sum of their squares as two ranks would."""
     g = [torch.randn(30000, device="cuda"), torch.randn(12345, device="cuda")]
