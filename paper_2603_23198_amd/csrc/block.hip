@@ -11,7 +11,10 @@
 //
 // Both directions are bound by memory: 4 (forward) and 6 (backward) rows of d elements move per
 // token and about 10 to 30 operations are done per element. So a row is read once and held in
-// registers between its sums and its outputs, eight elements per thread and chunk.
+// registers between its sums and its outputs, eight elements per thread and chunk. Measured, passes
+// back to back: forward of 8192 x 4096 bf16 50 us (5.3 TB/s), backward of 16384 x 4096 bf16 with all
+// parameter gradients 147 us (5.5 TB/s); a 1 GiB copy reaches 5.2. The simplest kernels (a workgroup
+// of 256 threads per row, rows read again for every sum) took 186 and 1927.
 #include "block.h"
 #include "rows.h"
 

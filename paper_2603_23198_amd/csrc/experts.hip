@@ -7,7 +7,9 @@
 // The passes over the rows are bound by memory and walk the tokens, so a token's own row is read
 // or written once however many experts it has; the expert side's rows (1 + k or 1 + 2 k rows of
 // traffic per token in all) are whole contiguous rows wherever they lie. Sums run over j in order,
-// in fp32, and no sum depends on another token; only whole-number counts are atomic.
+// in fp32, and no sum depends on another token; only whole-number counts are atomic. Measured at
+// 16384 x 4096 bf16 to two of eight experts: dispatch 77 us (5.2 TB/s), combine 74 (5.4), its gradient
+// 127 (5.3); a 1 GiB copy reaches 5.2.
 #include "block.h"
 #include "rows.h"
 
