@@ -75,7 +75,7 @@ def build(verbose=False, jobs=None, extra_flags=(), out=None, csrc=None) -> str:
     srcs = sorted(glob.glob(os.path.join(src_dir, "*.hip")) + glob.glob(os.path.join(src_dir, "*.cpp")))
     jobs = jobs or min(len(srcs), max(1, (os.cpu_count() or 4)), 16)
     with tempfile.TemporaryDirectory(prefix="sfl_build_") as tmp, cf.ThreadPoolExecutor(1) as side:
-        marshal = side.submit(build_marshal)
+        marshal = side.submit(build_marshal) if out is None else None
         objs = [os.path.join(tmp, os.path.basename(s) + ".o") for s in srcs]
         with cf.ThreadPoolExecutor(jobs) as ex:
             for src, msg in zip(srcs, ex.map(lambda a, o: _compile(a, o, extra_flags), srcs, objs)):
@@ -87,7 +87,8 @@ def build(verbose=False, jobs=None, extra_flags=(), out=None, csrc=None) -> str:
         if r.returncode != 0:
             raise RuntimeError(f"link failed:\n{r.stderr}")
         os.replace(tmp_lib, lib)
-        marshal.result()
+        if marshal:
+            marshal.result()
     return lib
 
 
