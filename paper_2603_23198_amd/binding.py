@@ -475,7 +475,7 @@ def grad_list(grads, out=None):
     the clipped gradients go, in place if None."""
     rows = _marshal.grads(grads, out)
     a = (Grad * len(grads)).from_buffer(rows) if rows else (Grad * 0)()
-    a._keepalive = (grads, out)
+    a._keepalive = (tuple(grads), None if out is None else tuple(out))  # the caller's lists may change
     return a
 
 
