@@ -537,7 +537,7 @@ typedef struct {
 sfl_status_t sfl_norm_forward(const sfl_norm_args_t* args, sfl_stream_t stream);
 sfl_status_t sfl_norm_backward(const sfl_norm_bwd_args_t* args, sfl_stream_t stream);
 
-/* Workspace bytes of sfl_norm_backward for rows of dtype. */
+/* Workspace bytes of sfl_norm_backward for rows of dtype, never more for fewer rows. */
 sfl_status_t sfl_norm_workspace_size(int64_t T, int64_t d, sfl_dtype_t dtype, size_t* bytes);
 
 /* Router: the k largest logits of each token and their softmax weights.
@@ -575,6 +575,7 @@ sfl_status_t sfl_route_backward(const void* logits, sfl_dtype_t dtype, int64_t T
 sfl_status_t sfl_expert_dispatch(const int32_t* expert, int64_t T, int32_t k, int32_t E, int32_t* pos,
                                  int32_t* offsets, const void* X, sfl_dtype_t dtype, int64_t d, int64_t rows, void* Xs,
                                  void* workspace, size_t workspace_bytes, sfl_stream_t stream);
+/* Never more for fewer tokens, choices or experts: the largest batch's serves all. */
 sfl_status_t sfl_expert_workspace_size(int64_t T, int32_t k, int32_t E, size_t* bytes);
 
 /* The experts' rows back to their tokens: Y[t] = sum_j weight[t][j] Ys[pos[t][j]], summed in fp32
@@ -613,6 +614,7 @@ typedef struct {
  * SFL_E_WORKSPACE. */
 sfl_status_t sfl_grad_sumsq(const sfl_grad_t* list, int32_t n, double* sumsq, void* workspace, size_t workspace_bytes,
                             sfl_stream_t stream);
+/* Never more for a part of a list or for shorter tensors. */
 sfl_status_t sfl_grad_workspace_size(const sfl_grad_t* list, int32_t n, size_t* bytes);
 
 /* Clipping by the global norm: norm[0] (fp32, device, may be NULL) = sqrt(*sumsq), and every

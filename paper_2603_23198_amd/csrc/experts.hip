@@ -223,7 +223,8 @@ __global__ __launch_bounds__(kOrderThreads) void k_expert_place(const int32_t* _
 
 // Slots of a workgroup: a tile of 1024, more where that would take over 256 workgroups (each adds
 // up the others' counts).
-int64_t order_run(int64_t n) { return cdiv(cdiv(n, 256), kOrderThreads) * kOrderThreads; }
+constexpr int kOrderBlocks = 256;
+int64_t order_run(int64_t n) { return cdiv(cdiv(n, kOrderBlocks), kOrderThreads) * kOrderThreads; }
 
 // -------------------------------------------------------------------------- the rows ----
 // NT threads per token, chunks of 8 columns each: as many threads as there are chunks, up to a
@@ -384,9 +385,11 @@ unsigned row_blocks(int64_t T, int nt) { return (unsigned)cdiv(T, kThreads / nt)
 
 }  // namespace
 
+// The counts of as many workgroups as n slots can take, not of those that they do take (with runs of
+// 2048 slots half as many as with 1024): a batch needs no more than a larger one.
 size_t expert_workspace_bytes(int64_t T, int k, int E) {
   const int64_t n = T * k;
-  return n <= kSmallSlots ? 0 : (size_t)cdiv(n, order_run(n)) * E * sizeof(int32_t);
+  return n <= kSmallSlots ? 0 : (size_t)std::min<int64_t>(cdiv(n, kOrderThreads), kOrderBlocks) * E * sizeof(int32_t);
 }
 
 hipError_t launch_expert_dispatch(const int32_t* expert, int64_t T, int k, int E, int32_t* pos, int32_t* offsets,

@@ -28,9 +28,10 @@ constexpr int kTile = 2048;      // smallest share of a workgroup
 // of 65536, 303 with 8192, 290 with 8192 and 4096; over 192 tensors 339 and 303), shorter ones too
 // (2048: 308 us). Short lists take smaller shares so that more CUs work.
 constexpr int kSumShare = 4 * kTile, kScaleShare = 2 * kTile;
+constexpr int64_t kFewShares = 1024;
 int64_t share_of(int64_t total, int64_t most) {
   int64_t share = kTile;
-  while (share < most && total / share > 1024) share *= 2;
+  while (share < most && total / share > kFewShares) share *= 2;
   return share;
 }
 
@@ -248,12 +249,18 @@ template <typename F> void with_list(const GradList<kListMax>& l, F f) {
 
 }  // namespace
 
-// A sum per workgroup; ranges of several tensors have at most as many as their tensors alone.
+// A sum per workgroup; ranges of several tensors have at most as many as their tensors alone. The
+// shares double as lists grow and the workgroups fall, so this counts those of the largest shares and
+// of any list whose shares are smaller (up to 1024, and one more per tensor): no list needs more than
+// one that holds it.
 size_t grad_workspace_bytes(const sfl_grad_t* list, int n) {
-  const int64_t share = share_of(elements(list, n), kSumShare);
-  int64_t blocks = 0;
-  for (int i = 0; i < n; ++i) blocks += cdiv(list[i].n, share);
-  return (size_t)blocks * sizeof(double);
+  int64_t smallest = 0, largest = 0, tensors = 0;
+  for (int i = 0; i < n; ++i) {
+    smallest += cdiv(list[i].n, kTile);
+    largest += cdiv(list[i].n, kSumShare);
+    tensors += list[i].n > 0;
+  }
+  return (size_t)std::max(largest, std::min(smallest, kFewShares + tensors)) * sizeof(double);
 }
 
 hipError_t launch_grad_sumsq(const sfl_grad_t* list, int n, double* sumsq, double* part, hipStream_t s) {
