@@ -383,7 +383,8 @@ def sfl_transpose(inp, out, stream=None):
 # ---- around the layer: norms, router, experts, gradient clipping ----
 # These take the tensors themselves, so shapes, types and contiguity are checked here.
 # Device pointer of a contiguous device tensor of n elements of a type (SFL_F32, SFL_BF16 or one of
-# the two below), None for None; ValueError for any other.
+# the two below), in rows of so many where a fourth argument says so; None for None; ValueError for
+# any other.
 _buf = _marshal.ptr
 _F32, _I32, _F64 = SFL_F32, 2, 3
 
@@ -396,9 +397,9 @@ def sfl_norm_forward(X, Y=None, *, X_out=None, N=None, norms=SFL_NORM_PRE | SFL_
                      gate_c=None, gate_t=None, res_scale=1.0, eps=1e-6, stream=None):
     T, d = X.shape
     dt, n = dtype_code(X.dtype), T * d
-    a = NormArgs(dt, norms, T, d, eps, res_scale, _buf(X, dt, n), _buf(Y, dt, n), _buf(w_pre, _F32, d),
-                 _buf(w_post, _F32, d), _buf(gate_c, _F32, d), _buf(gate_t, _F32, T), _buf(X_out, dt, n),
-                 _buf(N, dt, n))
+    a = NormArgs(dt, norms, T, d, eps, res_scale, _buf(X, dt, n, d), _buf(Y, dt, n, d), _buf(w_pre, _F32, d),
+                 _buf(w_post, _F32, d), _buf(gate_c, _F32, d), _buf(gate_t, _F32, T), _buf(X_out, dt, n, d),
+                 _buf(N, dt, n, d))
     _check("sfl_norm_forward", _lib.sfl_norm_forward(a, _stream(stream)))
 
 
@@ -414,26 +415,27 @@ def sfl_norm_backward(X_out, Y, dX_out, dN=None, *, dX=None, dY=None, dw_pre=Non
     like = X_out if X_out is not None else dX_out
     T, d = like.shape
     dt, n = dtype_code(like.dtype), T * d
-    a = NormBwdArgs(dt, norms, T, d, eps, res_scale, _buf(X_out, dt, n), _buf(Y, dt, n),
+    a = NormBwdArgs(dt, norms, T, d, eps, res_scale, _buf(X_out, dt, n, d), _buf(Y, dt, n, d),
                     _buf(w_pre, _F32, d), _buf(w_post, _F32, d), _buf(gate_c, _F32, d), _buf(gate_t, _F32, T),
-                    _buf(dX_out, dt, n), _buf(dN, dt, n), _buf(dX, dt, n), _buf(dY, dt, n), _buf(dw_pre, _F32, d),
-                    _buf(dw_post, _F32, d), _buf(dgate_c, _F32, d), _buf(dgate_t, _F32, T), *_space(workspace))
+                    _buf(dX_out, dt, n, d), _buf(dN, dt, n, d), _buf(dX, dt, n, d), _buf(dY, dt, n, d),
+                    _buf(dw_pre, _F32, d), _buf(dw_post, _F32, d), _buf(dgate_c, _F32, d), _buf(dgate_t, _F32, T),
+                    *_space(workspace))
     _check("sfl_norm_backward", _lib.sfl_norm_backward(a, _stream(stream)))
 
 
 def sfl_route_forward(logits, expert, weight, *, normalise=True, scale=1.0, stream=None):
     (T, E), k, dt = logits.shape, expert.shape[1], dtype_code(logits.dtype)
     _check("sfl_route_forward",
-           _lib.sfl_route_forward(_buf(logits, dt, T * E), dt, T, E, k, 1 if normalise else 0, scale,
-                                  _buf(expert, _I32, T * k), _buf(weight, _F32, T * k), _stream(stream)))
+           _lib.sfl_route_forward(_buf(logits, dt, T * E, E), dt, T, E, k, 1 if normalise else 0, scale,
+                                  _buf(expert, _I32, T * k, k), _buf(weight, _F32, T * k, k), _stream(stream)))
 
 
 def sfl_route_backward(logits, expert, dweight, dlogits, *, normalise=True, scale=1.0, stream=None):
     (T, E), k, dt = logits.shape, expert.shape[1], dtype_code(logits.dtype)
     _check("sfl_route_backward",
-           _lib.sfl_route_backward(_buf(logits, dt, T * E), dt, T, E, k, 1 if normalise else 0, scale,
-                                   _buf(expert, _I32, T * k), _buf(dweight, _F32, T * k), _buf(dlogits, dt, T * E),
-                                   _stream(stream)))
+           _lib.sfl_route_backward(_buf(logits, dt, T * E, E), dt, T, E, k, 1 if normalise else 0, scale,
+                                   _buf(expert, _I32, T * k, k), _buf(dweight, _F32, T * k, k),
+                                   _buf(dlogits, dt, T * E, E), _stream(stream)))
 
 
 def sfl_expert_workspace_size(T, k, E):
@@ -447,27 +449,27 @@ def sfl_expert_dispatch(expert, E, pos, offsets, *, X=None, Xs=None, workspace=N
     n, dt, d, rows, px, ps = T * k, SFL_F32, 1, 0, None, None
     if X is not None:
         d, rows, dt = X.shape[1], Xs.shape[0], dtype_code(X.dtype)
-        px, ps = _buf(X, dt, T * d), _buf(Xs, dt, rows * d)
+        px, ps = _buf(X, dt, T * d, d), _buf(Xs, dt, rows * d, d)
     ws, ws_bytes = _space(workspace)
     _check("sfl_expert_dispatch",
-           _lib.sfl_expert_dispatch(_buf(expert, _I32, n), T, k, E, _buf(pos, _I32, n), _buf(offsets, _I32, E + 1), px,
-                                    dt, d, rows, ps, ws, ws_bytes, _stream(stream)))
+           _lib.sfl_expert_dispatch(_buf(expert, _I32, n, k), T, k, E, _buf(pos, _I32, n, k),
+                                    _buf(offsets, _I32, E + 1), px, dt, d, rows, ps, ws, ws_bytes, _stream(stream)))
 
 
 def sfl_expert_combine(Ys, pos, Y, *, weight=None, stream=None):
     (T, k), (rows, d), dt = pos.shape, Ys.shape, dtype_code(Ys.dtype)
     _check("sfl_expert_combine",
-           _lib.sfl_expert_combine(_buf(Ys, dt, rows * d), dt, T, d, k, _buf(pos, _I32, T * k), rows,
-                                   _buf(weight, _F32, T * k), _buf(Y, dt, T * d), _stream(stream)))
+           _lib.sfl_expert_combine(_buf(Ys, dt, rows * d, d), dt, T, d, k, _buf(pos, _I32, T * k, k), rows,
+                                   _buf(weight, _F32, T * k, k), _buf(Y, dt, T * d, d), _stream(stream)))
 
 
 def sfl_expert_combine_backward(dY, Ys, pos, weight, *, dYs=None, dweight=None, stream=None):
     (T, k), d, dt = pos.shape, dY.shape[1], dtype_code(dY.dtype)
     rows = (dYs if Ys is None else Ys).shape[0]
     _check("sfl_expert_combine_backward",
-           _lib.sfl_expert_combine_backward(_buf(dY, dt, T * d), _buf(Ys, dt, rows * d), dt, T, d, k,
-                                            _buf(pos, _I32, T * k), rows, _buf(weight, _F32, T * k),
-                                            _buf(dYs, dt, rows * d), _buf(dweight, _F32, T * k), _stream(stream)))
+           _lib.sfl_expert_combine_backward(_buf(dY, dt, T * d, d), _buf(Ys, dt, rows * d, d), dt, T, d, k,
+                                            _buf(pos, _I32, T * k, k), rows, _buf(weight, _F32, T * k, k),
+                                            _buf(dYs, dt, rows * d, d), _buf(dweight, _F32, T * k, k), _stream(stream)))
 
 
 def grad_list(grads, out=None):

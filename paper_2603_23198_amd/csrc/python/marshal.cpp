@@ -19,9 +19,17 @@ bool is_kind(const at::Tensor& t, long kind) {
   }
 }
 
+// Whether the tensor is rows of `cols` elements: trailing dimensions of it, the first not among them,
+// hold that many ([batch][token][cols] and [token][head][cols / heads] do), or it is flat.
+bool in_rows(const at::Tensor& t, int64_t cols) {
+  int64_t n = 1;
+  for (int64_t i = t.dim() - 1; i > 0 && n != cols; --i) n *= t.size(i);
+  return n == cols || t.dim() < 2;
+}
+
 // The tensor's pointer if it is a contiguous device tensor of the kind and n elements (any number
-// where n < 0); else false with a Python error set.
-bool pointer(PyObject* o, long kind, long long n, const void** p, int64_t* numel) {
+// where n < 0) in rows of cols (any where cols < 0); else false with a Python error set.
+bool pointer(PyObject* o, long kind, long long n, long long cols, const void** p, int64_t* numel) {
   if (!THPVariable_Check(o)) {
     PyErr_Format(PyExc_TypeError, "expected a tensor, got %.80s", Py_TYPE(o)->tp_name);
     return false;
@@ -31,6 +39,11 @@ bool pointer(PyObject* o, long kind, long long n, const void** p, int64_t* numel
     PyErr_Format(PyExc_ValueError, "expected a contiguous %s tensor of %lld elements on the GPU, got %s of %lld%s%s",
                  kNames[kind], n >= 0 ? n : (long long)t.numel(), at::toString(t.scalar_type()), (long long)t.numel(),
                  t.is_contiguous() ? "" : ", not contiguous", t.is_cuda() ? "" : ", on the CPU");
+    return false;
+  }
+  if (cols >= 0 && !in_rows(t, cols)) {
+    PyErr_Format(PyExc_ValueError, "expected rows of %lld elements, got a last dimension of %lld", cols,
+                 (long long)t.size(-1));
     return false;
   }
   *p = t.numel() ? t.data_ptr() : nullptr;
@@ -48,16 +61,16 @@ template <typename F> PyObject* guarded(F f) {
   }
 }
 
-// ptr(tensor or None, kind, n) -> device pointer or None
+// ptr(tensor or None, kind, n[, cols]) -> device pointer or None
 PyObject* ptr(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   return guarded([&]() -> PyObject* {
-    if (nargs != 3) {
-      PyErr_SetString(PyExc_TypeError, "ptr(tensor, kind, n)");
+    if (nargs != 3 && nargs != 4) {
+      PyErr_SetString(PyExc_TypeError, "ptr(tensor, kind, n[, cols])");
       return nullptr;
     }
     if (a[0] == Py_None) Py_RETURN_NONE;
     const long kind = PyLong_AsLong(a[1]);
-    const long long n = PyLong_AsLongLong(a[2]);
+    const long long n = PyLong_AsLongLong(a[2]), cols = nargs == 4 ? PyLong_AsLongLong(a[3]) : -1;
     if (PyErr_Occurred()) return nullptr;
     if (kind < 0 || kind > 3) {
       PyErr_SetString(PyExc_ValueError, "unknown kind of tensor");
@@ -65,7 +78,7 @@ PyObject* ptr(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     }
     const void* p;
     int64_t numel;
-    if (!pointer(a[0], kind, n, &p, &numel)) return nullptr;
+    if (!pointer(a[0], kind, n, cols, &p, &numel)) return nullptr;
     return PyLong_FromVoidPtr(const_cast<void*>(p));
   });
 }
@@ -92,8 +105,8 @@ PyObject* grads(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
       const void *src = nullptr, *dst = nullptr;
       int64_t numel = 0, out_numel = 0;
       const long kind = THPVariable_Check(o) && THPVariable_Unpack(o).scalar_type() == at::kBFloat16 ? SFL_BF16 : SFL_F32;
-      if (!pointer(o, kind, -1, &src, &numel) ||
-          (has_out && !pointer(PySequence_Fast_GET_ITEM(a[1], i), kind, numel, &dst, &out_numel))) {
+      if (!pointer(o, kind, -1, -1, &src, &numel) ||
+          (has_out && !pointer(PySequence_Fast_GET_ITEM(a[1], i), kind, numel, -1, &dst, &out_numel))) {
         Py_DECREF(rows);
         return nullptr;
       }

@@ -111,3 +111,20 @@ def test_a_refusal_says_what_it_wanted():
         with pytest.raises(ValueError, match=says):
             b.sfl_norm_forward(x, bad, X_out=x, N=n)
     b.sfl_norm_forward(x, new(T, D), X_out=x, N=n)
+
+
+@pytest.mark.parametrize("make", CALLS[:-1], ids=lambda f: f.__name__)
+def test_rows_of_another_width(make):
+    """As many elements, in rows of another width: [d][T] is not [T][d]. Rows that are
+    counted or divided by several dimensions and flat buffers have the same order in memory and are taken."""
+    tensors, call = make()
+    for name, t in tensors.items():
+        if t.dim() != 2 or (name in GIVES_SIZES and (make, name) != (dispatch, "pos")):
+            continue
+        for bad in (t.view(t.shape[1], t.shape[0]), t.view(2, -1, t.shape[1] // 2), t.view(1, -1)):
+            with pytest.raises(ValueError):
+                call(**{**tensors, name: bad})
+                pytest.fail(f"{make.__name__} took {name} as {tuple(bad.shape)}")
+        for good in (t.view(2, -1, t.shape[1]), t.view(t.shape[0], 2, -1), t.view(-1)):
+            call(**{**tensors, name: good})
+    torch.cuda.synchronize()
