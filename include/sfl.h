@@ -532,8 +532,8 @@ typedef struct {
 } sfl_norm_bwd_args_t;
 
 /* Errors of both: SFL_E_ARG for bad sizes, unknown norm bits, eps below 0 or NaN, a NULL buffer
- * that the call needs (T > 0) or one given that has no meaning (see above); SFL_E_UNSUPPORTED for
- * d > 16384; SFL_E_WORKSPACE. T = 0 does nothing but clear the parameters' gradients. */
+ * that the call needs (T > 0), one given that has no meaning (see above) or a misaligned workspace;
+ * SFL_E_UNSUPPORTED for d > 16384; SFL_E_WORKSPACE. T = 0 does nothing but clear the parameters' gradients. */
 sfl_status_t sfl_norm_forward(const sfl_norm_args_t* args, sfl_stream_t stream);
 sfl_status_t sfl_norm_backward(const sfl_norm_bwd_args_t* args, sfl_stream_t stream);
 
@@ -570,8 +570,8 @@ sfl_status_t sfl_route_backward(const void* logits, sfl_dtype_t dtype, int64_t T
  *          on are left as they are (rows = T k always suffices).
  *  workspace  sfl_expert_workspace_size() bytes, 4-byte aligned (may be NULL when that is 0)
  * 1 <= E <= 1024, 1 <= k <= 64. Errors: SFL_E_ARG for bad sizes, NULL buffers (T > 0; offsets
- * always) or only one of X and Xs (Xs may be NULL with rows = 0); SFL_E_UNSUPPORTED for E > 1024,
- * k > 64, T k > 2^31 - 1 or d > 2^30; SFL_E_WORKSPACE. */
+ * always), only one of X and Xs (Xs may be NULL with rows = 0) or a misaligned workspace;
+ * SFL_E_UNSUPPORTED for E > 1024, k > 64, T k > 2^31 - 1 or d > 2^30; SFL_E_WORKSPACE. */
 sfl_status_t sfl_expert_dispatch(const int32_t* expert, int64_t T, int32_t k, int32_t E, int32_t* pos,
                                  int32_t* offsets, const void* X, sfl_dtype_t dtype, int64_t d, int64_t rows, void* Xs,
                                  void* workspace, size_t workspace_bytes, sfl_stream_t stream);
@@ -610,8 +610,8 @@ typedef struct {
  * empty list). Formed in fp64: it neither overflows nor underflows for finite gradients. Ranks
  * that hold parts of the gradients add their sums before they clip. workspace:
  * sfl_grad_workspace_size() bytes, 8-byte aligned. Errors: SFL_E_ARG for n < 0, a NULL list (n > 0)
- * or sumsq, an element count below 0, an unknown dtype or a NULL src with elements;
- * SFL_E_WORKSPACE. */
+ * or sumsq, an element count below 0, an unknown dtype, a NULL src with elements or a misaligned
+ * workspace; SFL_E_WORKSPACE. */
 sfl_status_t sfl_grad_sumsq(const sfl_grad_t* list, int32_t n, double* sumsq, void* workspace, size_t workspace_bytes,
                             sfl_stream_t stream);
 /* Never more for a part of a list or for shorter tensors. */

@@ -386,11 +386,8 @@ def sfl_transpose(inp, out, stream=None):
 # the two below), in rows of so many where a fourth argument says so; None for None; ValueError for
 # any other.
 _buf = _marshal.ptr
+_space = _marshal.space  # (device pointer, bytes) of a contiguous device tensor, or (None, 0) for None
 _F32, _I32, _F64 = SFL_F32, 2, 3
-
-
-def _space(workspace):
-    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
 
 
 def sfl_norm_forward(X, Y=None, *, X_out=None, N=None, norms=SFL_NORM_PRE | SFL_NORM_POST, w_pre=None, w_post=None,

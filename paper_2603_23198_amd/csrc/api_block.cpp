@@ -17,6 +17,13 @@ bool dtype_ok(int32_t t) { return t == SFL_F32 || t == SFL_BF16; }
 // Rows times width stays within the 64-bit byte offsets of the kernels.
 bool size_ok(int64_t rows, int64_t d) { return rows >= 0 && d >= 1 && rows <= ((int64_t)1 << 60) / d; }
 
+// A workspace of `need` bytes that holds values of `align` bytes.
+sfl_status_t check_space(const void* workspace, size_t bytes, size_t need, size_t align) {
+  if (need == 0) return SFL_OK;
+  if (!workspace || bytes < need) return SFL_E_WORKSPACE;
+  return (uintptr_t)workspace % align ? SFL_E_ARG : SFL_OK;
+}
+
 sfl_status_t status(hipError_t e) { return e == hipSuccess ? SFL_OK : SFL_E_HIP; }
 
 sfl_status_t check_norm(sfl_dtype_t dtype, int32_t norms, int64_t T, int64_t d, float eps, const void* Y,
@@ -97,7 +104,7 @@ sfl_status_t sfl_norm_workspace_size(int64_t T, int64_t d, sfl_dtype_t dtype, si
 
 sfl_status_t sfl_norm_backward(const sfl_norm_bwd_args_t* a, sfl_stream_t stream) {
   if (!a) return SFL_E_ARG;
-  const sfl_status_t st =
+  sfl_status_t st =
       check_norm(a->dtype, a->norms, a->T, a->d, a->eps, a->Y, a->w_pre, a->w_post, a->gate_c, a->gate_t);
   if (st != SFL_OK) return st;
   const bool pre = a->norms & SFL_NORM_PRE, post = a->norms & SFL_NORM_POST;
@@ -105,7 +112,8 @@ sfl_status_t sfl_norm_backward(const sfl_norm_bwd_args_t* a, sfl_stream_t stream
   if (a->dw_post && !post) return SFL_E_ARG;
   if (a->T > 0 && ((pre && !a->X_out) || (!a->Y && (a->dY || a->dgate_c || a->dgate_t)))) return SFL_E_ARG;
   const size_t need = norm_workspace_bytes(a->T, a->d, a->dtype == SFL_BF16);
-  if (need > 0 && (!a->workspace || a->workspace_bytes < need)) return SFL_E_WORKSPACE;
+  st = check_space(a->workspace, a->workspace_bytes, need, sizeof(float));
+  if (st != SFL_OK) return st;
   NormBwdParams p{};
   p.T = a->T;
   p.d = a->d;
@@ -162,13 +170,13 @@ sfl_status_t sfl_expert_workspace_size(int64_t T, int32_t k, int32_t E, size_t* 
 sfl_status_t sfl_expert_dispatch(const int32_t* expert, int64_t T, int32_t k, int32_t E, int32_t* pos,
                                  int32_t* offsets, const void* X, sfl_dtype_t dtype, int64_t d, int64_t rows, void* Xs,
                                  void* workspace, size_t workspace_bytes, sfl_stream_t stream) {
-  const sfl_status_t st = check_rows(dtype, T, d, k, rows);
+  sfl_status_t st = check_rows(dtype, T, d, k, rows);
   if (st != SFL_OK) return st;
   if (E < 1 || !offsets) return SFL_E_ARG;
   if (E > kRouteMaxExperts) return SFL_E_UNSUPPORTED;
   if (T > 0 && (!expert || !pos || (X && !Xs && rows > 0) || (Xs && !X))) return SFL_E_ARG;
-  const size_t need = expert_workspace_bytes(T, k, E);
-  if (need > 0 && (!workspace || workspace_bytes < need)) return SFL_E_WORKSPACE;
+  st = check_space(workspace, workspace_bytes, expert_workspace_bytes(T, k, E), sizeof(int32_t));
+  if (st != SFL_OK) return st;
   return status(launch_expert_dispatch(expert, T, k, E, pos, offsets, X, dtype == SFL_BF16, d, rows, Xs, workspace,
                                        (hipStream_t)stream));
 }
@@ -201,11 +209,11 @@ sfl_status_t sfl_grad_workspace_size(const sfl_grad_t* list, int32_t n, size_t* 
 
 sfl_status_t sfl_grad_sumsq(const sfl_grad_t* list, int32_t n, double* sumsq, void* workspace, size_t workspace_bytes,
                             sfl_stream_t stream) {
-  const sfl_status_t st = check_grads(list, n);
+  sfl_status_t st = check_grads(list, n);
   if (st != SFL_OK) return st;
   if (!sumsq) return SFL_E_ARG;
-  const size_t need = grad_workspace_bytes(list, n);
-  if (need > 0 && (!workspace || workspace_bytes < need)) return SFL_E_WORKSPACE;
+  st = check_space(workspace, workspace_bytes, grad_workspace_bytes(list, n), sizeof(double));
+  if (st != SFL_OK) return st;
   return status(launch_grad_sumsq(list, n, sumsq, (double*)workspace, (hipStream_t)stream));
 }
 

@@ -83,6 +83,25 @@ PyObject* ptr(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   });
 }
 
+// space(tensor or None) -> (device pointer or None, bytes) of a workspace of any type
+PyObject* space(PyObject*, PyObject* o) {
+  return guarded([&]() -> PyObject* {
+    if (o == Py_None) return Py_BuildValue("(Oi)", Py_None, 0);
+    if (!THPVariable_Check(o)) {
+      PyErr_Format(PyExc_TypeError, "expected a tensor as workspace, got %.80s", Py_TYPE(o)->tp_name);
+      return nullptr;
+    }
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_contiguous() || !t.is_cuda()) {
+      PyErr_Format(PyExc_ValueError, "expected a contiguous workspace on the GPU, got one that is%s%s",
+                   t.is_contiguous() ? "" : " not contiguous", t.is_cuda() ? "" : " on the CPU");
+      return nullptr;
+    }
+    if (!t.numel()) return Py_BuildValue("(Oi)", Py_None, 0);
+    return Py_BuildValue("(NK)", PyLong_FromVoidPtr(t.data_ptr()), (unsigned long long)t.nbytes());
+  });
+}
+
 // grads(sequence of tensors, sequence of as many or None) -> bytearray of sfl_grad_t
 PyObject* grads(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   return guarded([&]() -> PyObject* {
@@ -117,6 +136,7 @@ PyObject* grads(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
 }
 
 PyMethodDef methods[] = {{"ptr", (PyCFunction)(void (*)(void))ptr, METH_FASTCALL, nullptr},
+                         {"space", space, METH_O, nullptr},
                          {"grads", (PyCFunction)(void (*)(void))grads, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};

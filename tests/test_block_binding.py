@@ -28,3 +28,13 @@ def test_a_list_of_gradients_keeps_its_tensors(monkeypatch, kind):
     del handle
     gc.collect()
     assert all(r() is None for r in held)
+
+
+def test_a_workspace_that_the_kernels_cannot_use_is_refused():
+    with pytest.raises(ValueError, match="on the CPU"):
+        b._space(torch.empty(64, dtype=torch.uint8))
+    with pytest.raises(ValueError, match="not contiguous"):
+        b._space(torch.empty((8, 8), dtype=torch.uint8).t()[1:])
+    with pytest.raises(TypeError):
+        b._space(0x1000)
+    assert b._space(None) == (None, 0)

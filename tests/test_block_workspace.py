@@ -50,3 +50,23 @@ def test_norms(dt):
     for d in (1, 64, 130, 640, 1003, 4096, 8200, 16384):
         sizes = [b.sfl_norm_workspace_size(T, d, dt) for T in (*range(0, 70), 511, 512, 513, 8191, 8192, 8193, 1 << 20)]
         assert sizes == sorted(sizes), d
+
+
+def test_alignment():
+    """Workspaces hold fp32 sums, int32 counts and fp64 sums: 4, 4 and 8 bytes."""
+    norm = b.NormBwdArgs()
+    norm.dtype, norm.norms, norm.T, norm.d, norm.eps, norm.res_scale = b.SFL_BF16, 3, 4, 64, 1e-6, 1.0
+    norm.X_out = norm.Y = norm.dX_out = norm.dN = norm.dX = P
+    norm.workspace_bytes = 1 << 30
+    one = (b.Grad * 1)((P, None, 10, 0, 0))
+    for by in (1, 2, 3):
+        norm.workspace = P + by
+        assert b._lib.sfl_norm_backward(norm, None) == b.SFL_E_ARG
+        assert b._lib.sfl_expert_dispatch(P, 16384, 8, 64, P, P, None, 0, 1, 0, None, P + by, 1 << 30, None) == b.SFL_E_ARG
+    for by in range(1, 8):
+        assert b._lib.sfl_grad_sumsq(one, 1, P, P + by, 1 << 20, None) == b.SFL_E_ARG
+
+
+def test_a_workspace_that_is_not_needed_may_lie_anywhere():
+    """(On the CPU the launch itself is what fails.)"""
+    assert b._lib.sfl_expert_dispatch(P, 4, 2, 8, P, P, None, 0, 1, 0, None, None, 0, None) != b.SFL_E_ARG
