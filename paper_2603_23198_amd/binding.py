@@ -410,6 +410,10 @@ def sfl_norm_backward(X_out, Y, dX_out, dN=None, *, dX=None, dY=None, dw_pre=Non
                       dgate_t=None, norms=SFL_NORM_PRE | SFL_NORM_POST, w_pre=None, w_post=None, gate_c=None,
                       gate_t=None, res_scale=1.0, eps=1e-6, workspace=None, stream=None):
     like = X_out if X_out is not None else dX_out
+    if like is None:
+        like = next((t for t in (Y, dN, dX) if t is not None), None)
+    if like is None:
+        raise ValueError("sfl_norm_backward: no tensor of rows gives the sizes")
     T, d = like.shape
     dt, n = dtype_code(like.dtype), T * d
     a = NormBwdArgs(dt, norms, T, d, eps, res_scale, _buf(X_out, dt, n, d), _buf(Y, dt, n, d),
@@ -444,8 +448,9 @@ def sfl_expert_workspace_size(T, k, E):
 def sfl_expert_dispatch(expert, E, pos, offsets, *, X=None, Xs=None, workspace=None, stream=None):
     T, k = expert.shape
     n, dt, d, rows, px, ps = T * k, SFL_F32, 1, 0, None, None
-    if X is not None:
-        d, rows, dt = X.shape[1], Xs.shape[0], dtype_code(X.dtype)
+    like = X if X is not None else Xs
+    if like is not None:  # one of the two alone is for the entry point to judge
+        d, rows, dt = like.shape[1], 0 if Xs is None else Xs.shape[0], dtype_code(like.dtype)
         px, ps = _buf(X, dt, T * d, d), _buf(Xs, dt, rows * d, d)
     ws, ws_bytes = _space(workspace)
     _check("sfl_expert_dispatch",
@@ -462,7 +467,10 @@ def sfl_expert_combine(Ys, pos, Y, *, weight=None, stream=None):
 
 def sfl_expert_combine_backward(dY, Ys, pos, weight, *, dYs=None, dweight=None, stream=None):
     (T, k), d, dt = pos.shape, dY.shape[1], dtype_code(dY.dtype)
-    rows = (dYs if Ys is None else Ys).shape[0]
+    like = dYs if Ys is None else Ys
+    if like is None and dweight is not None:
+        raise ValueError("sfl_expert_combine_backward: dweight needs Ys")
+    rows = 0 if like is None else like.shape[0]
     _check("sfl_expert_combine_backward",
            _lib.sfl_expert_combine_backward(_buf(dY, dt, T * d, d), _buf(Ys, dt, rows * d, d), dt, T, d, k,
                                             _buf(pos, _I32, T * k, k), rows, _buf(weight, _F32, T * k, k),
