@@ -4,7 +4,9 @@ Every function here has the name of the C entry point it calls and forwards
 device pointers (torch tensors' data_ptr()) and the current HIP stream; the operators
 around the layer also check the tensors' types, sizes and contiguity. All
 arithmetic happens in the HIP kernels of libsfl.so; if the library is missing
-or fails to load, importing this module raises (there is no fallback path).
+or fails to load, importing this module raises (there is no fallback path). The
+extension module `_marshal.so` turns tensors into checked pointers for the operators
+around the layer, and only those need it.
 """
 from __future__ import annotations
 
@@ -22,7 +24,25 @@ if not os.path.exists(LIB_PATH):
                       "`python -m paper_2603_23198_amd.build` (or __graft_entry__.build())")
 _lib = ctypes.CDLL(LIB_PATH)
 
-from . import _marshal  # noqa: E402  (built beside libsfl.so)
+
+class _NotBuilt:
+    """Stands for the extension module `_marshal` where it cannot be loaded: the layer's entry points
+    do without it, those that take checked tensors raise ImportError."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def ptr(self, *_):
+        raise ImportError(f"the binding's extension module _marshal.so cannot be loaded ({self._why}); build it with "
+                          "`python -m paper_2603_23198_amd.build` (or __graft_entry__.build())")
+
+    space = grads = ptr
+
+
+try:
+    from . import _marshal
+except ImportError as e:
+    _marshal = _NotBuilt(e)
 
 SFL_F32, SFL_BF16 = 0, 1
 SFL_OK, SFL_E_ARG, SFL_E_UNSUPPORTED, SFL_E_WORKSPACE, SFL_E_HIP = 0, -1, -2, -3, -4
