@@ -8,6 +8,7 @@ into `libsfl.so` next to this file. The build always recompiles (it is the
 from __future__ import annotations
 
 import concurrent.futures as cf
+import contextlib
 import glob
 import os
 import shutil
@@ -50,8 +51,18 @@ def _compile(src, obj, extra=()):
     return errs
 
 
-def build_marshal() -> str:
-    """Compile the binding's extension module against the installed torch (host code only)."""
+@contextlib.contextmanager
+def _beside(path):
+    """A temporary name beside `path`, to be moved there when it is complete."""
+    tmp = path + ".tmp"
+    try:
+        yield tmp
+    finally:
+        if os.path.exists(tmp):
+            os.remove(tmp)
+
+
+def _compile_marshal(out):
     import torch
     at = os.path.dirname(torch.__file__)
     cxx = shutil.which("g++") or shutil.which("c++") or hipcc()
@@ -59,36 +70,43 @@ def build_marshal() -> str:
            "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(at, "include"),
            "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
            os.path.join(CSRC, "python", "marshal.cpp"), "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu",
-           "-lc10", "-Wl,-rpath," + os.path.join(at, "lib"), "-o", MARSHAL + ".tmp"]
+           "-lc10", "-Wl,-rpath," + os.path.join(at, "lib"), "-o", out]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"compiling marshal.cpp failed:\n{r.stderr}")
-    os.replace(MARSHAL + ".tmp", MARSHAL)
+
+
+def build_marshal() -> str:
+    """Compile the binding's extension module against the installed torch (host code only)."""
+    with _beside(MARSHAL) as tmp:
+        _compile_marshal(tmp)
+        os.replace(tmp, MARSHAL)
     return MARSHAL
 
 
 def build(verbose=False, jobs=None, extra_flags=(), out=None, csrc=None) -> str:
     """Compile and link; `extra_flags` go to every hipcc line, `out` overrides the library
-    path and `csrc` the source directory."""
+    path and `csrc` the source directory. Nothing is replaced unless everything was built."""
     lib = out or LIB
     src_dir = csrc or CSRC
     srcs = sorted(glob.glob(os.path.join(src_dir, "*.hip")) + glob.glob(os.path.join(src_dir, "*.cpp")))
     jobs = jobs or min(len(srcs), max(1, (os.cpu_count() or 4)), 16)
-    with tempfile.TemporaryDirectory(prefix="sfl_build_") as tmp, cf.ThreadPoolExecutor(1) as side:
-        marshal = side.submit(build_marshal) if out is None else None
+    with tempfile.TemporaryDirectory(prefix="sfl_build_") as tmp, _beside(lib) as tmp_lib, \
+            _beside(MARSHAL) as tmp_marshal, cf.ThreadPoolExecutor(1) as side:
+        marshal = side.submit(_compile_marshal, tmp_marshal) if out is None else None
         objs = [os.path.join(tmp, os.path.basename(s) + ".o") for s in srcs]
         with cf.ThreadPoolExecutor(jobs) as ex:
             for src, msg in zip(srcs, ex.map(lambda a, o: _compile(a, o, extra_flags), srcs, objs)):
                 if verbose and msg.strip():
                     print(f"[{os.path.basename(src)}]\n{msg}", file=sys.stderr)
-        tmp_lib = lib + ".tmp"
         cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp_lib]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"link failed:\n{r.stderr}")
-        os.replace(tmp_lib, lib)
         if marshal:
             marshal.result()
+            os.replace(tmp_marshal, MARSHAL)
+        os.replace(tmp_lib, lib)
     return lib
 
 

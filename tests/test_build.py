@@ -49,3 +49,54 @@ print("ran to the end")
     assert r.returncode == 0, r.stderr
     lines = r.stdout.split("\n")
     assert lines[0].startswith(str(tmp_path)) and lines[1] == "ran to the end"
+
+
+@pytest.fixture
+def targets(tmp_path, monkeypatch):
+    """Build targets with old contents, and a source directory that compiles in a moment."""
+    try:
+        build.hipcc()
+    except RuntimeError:
+        pytest.skip("no hipcc")
+    for name in ("LIB", "MARSHAL"):
+        (tmp_path / name).write_text("old")
+        monkeypatch.setattr(build, name, str(tmp_path / name))
+    src = tmp_path / "csrc"
+    src.mkdir()
+    (src / "one.cpp").write_text('extern "C" int one() { return 1; }\n')
+    return tmp_path, src
+
+
+def contents(path):
+    return {p.name: p.read_bytes() == b"old" for p in path.iterdir() if p.is_file()}
+
+
+def broken_command(monkeypatch, part):
+    """The compiler's command line that has `part` in it gets an option that does not exist."""
+    run = subprocess.run
+
+    def run_or_break(cmd, **kw):
+        return run([*cmd, "-fno-such-option-at-all"] if any(part in c for c in cmd) else cmd, **kw)
+
+    monkeypatch.setattr(build.subprocess, "run", run_or_break)
+
+
+@pytest.mark.parametrize("part", ["marshal.cpp", "one.cpp", "one.cpp.o"])
+def test_a_failed_build_leaves_both_files_as_they_were(targets, monkeypatch, part):
+    path, src = targets
+    broken_command(monkeypatch, part)
+    with pytest.raises(RuntimeError, match="failed"):
+        build.build(csrc=str(src))
+    assert contents(path) == {"LIB": True, "MARSHAL": True}
+
+
+def test_a_build_replaces_both_files(targets):
+    path, src = targets
+    assert build.build(csrc=str(src)) == str(path / "LIB")
+    assert contents(path) == {"LIB": False, "MARSHAL": False}
+
+
+def test_a_library_elsewhere_leaves_the_extension_module(targets):
+    path, src = targets
+    build.build(csrc=str(src), out=str(path / "other"))
+    assert contents(path) == {"LIB": True, "MARSHAL": True, "other": False}
