@@ -92,6 +92,9 @@ __device__ __forceinline__ int wave_incl_scan(int v) {
   return v;
 }
 
+// Workgroups of so many threads that one launch takes: its work items stay below 2^32.
+constexpr int64_t max_blocks(int threads) { return (((int64_t)1 << 32) - 1) / threads; }
+
 __host__ __device__ constexpr int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace sfl

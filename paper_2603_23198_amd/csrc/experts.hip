@@ -381,7 +381,19 @@ template <typename F> hipError_t with_threads(int64_t d, int k, F f) {
   return hipErrorInvalidValue;
 }
 
-unsigned row_blocks(int64_t T, int nt) { return (unsigned)cdiv(T, kThreads / nt); }
+// Calls f with a first token, a number of tokens and their workgroups, for as many tokens at a time
+// as one launch takes (2^24 - 1 where each has a workgroup of its own).
+template <int NT, typename F> hipError_t over_tokens(int64_t T, F f) {
+  constexpr int per = kThreads / NT;
+  constexpr int64_t most = max_blocks(kThreads) * per;
+  for (int64_t t0 = 0; t0 < T; t0 += most) {
+    const int64_t n = std::min(T - t0, most);
+    f(t0, n, dim3((unsigned)cdiv(n, per)));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 
 }  // namespace
 
@@ -421,13 +433,14 @@ hipError_t launch_expert_dispatch(const int32_t* expert, int64_t T, int k, int E
   if (!X || rows == 0) return hipGetLastError();
   return with_threads(d, k, [&](auto nt, auto) {
     constexpr int NT = decltype(nt)::value;
-    if (bf16)
-      hipLaunchKernelGGL((k_expert_rows<bf16_t, NT>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s, (const bf16_t*)X, T,
-                         d, k, pos, rows, (bf16_t*)Xs);
-    else
-      hipLaunchKernelGGL((k_expert_rows<float, NT>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s, (const float*)X, T,
-                         d, k, pos, rows, (float*)Xs);
-    return hipGetLastError();
+    return over_tokens<NT>(T, [&](int64_t t0, int64_t n, dim3 grid) {
+      if (bf16)
+        hipLaunchKernelGGL((k_expert_rows<bf16_t, NT>), grid, dim3(kThreads), 0, s, (const bf16_t*)X + t0 * d, n, d, k,
+                           pos + t0 * k, rows, (bf16_t*)Xs);
+      else
+        hipLaunchKernelGGL((k_expert_rows<float, NT>), grid, dim3(kThreads), 0, s, (const float*)X + t0 * d, n, d, k,
+                           pos + t0 * k, rows, (float*)Xs);
+    });
   });
 }
 
@@ -435,13 +448,15 @@ hipError_t launch_expert_combine(const void* Ys, int bf16, int64_t T, int64_t d,
                                  int64_t rows, const float* weight, void* Y, hipStream_t s) {
   return with_threads(d, k, [&](auto nt, auto ks) {
     constexpr int NT = decltype(nt)::value, KS = decltype(ks)::value;
-    if (bf16)
-      hipLaunchKernelGGL((k_expert_combine<bf16_t, NT, KS>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s,
-                         (const bf16_t*)Ys, T, d, k, pos, rows, weight, (bf16_t*)Y);
-    else
-      hipLaunchKernelGGL((k_expert_combine<float, NT, KS>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s, (const float*)Ys,
-                         T, d, k, pos, rows, weight, (float*)Y);
-    return hipGetLastError();
+    return over_tokens<NT>(T, [&](int64_t t0, int64_t n, dim3 grid) {
+      const float* w = weight ? weight + t0 * k : nullptr;
+      if (bf16)
+        hipLaunchKernelGGL((k_expert_combine<bf16_t, NT, KS>), grid, dim3(kThreads), 0, s, (const bf16_t*)Ys, n, d, k,
+                           pos + t0 * k, rows, w, (bf16_t*)Y + t0 * d);
+      else
+        hipLaunchKernelGGL((k_expert_combine<float, NT, KS>), grid, dim3(kThreads), 0, s, (const float*)Ys, n, d, k,
+                           pos + t0 * k, rows, w, (float*)Y + t0 * d);
+    });
   });
 }
 
@@ -450,13 +465,16 @@ hipError_t launch_expert_combine_bwd(const void* dY, const void* Ys, int bf16, i
                                      hipStream_t s) {
   return with_threads(d, k, [&](auto nt, auto ks) {
     constexpr int NT = decltype(nt)::value, KS = decltype(ks)::value;
-    if (bf16)
-      hipLaunchKernelGGL((k_expert_combine_bwd<bf16_t, NT, KS>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s,
-                         (const bf16_t*)dY, (const bf16_t*)Ys, T, d, k, pos, rows, weight, (bf16_t*)dYs, dweight);
-    else
-      hipLaunchKernelGGL((k_expert_combine_bwd<float, NT, KS>), dim3(row_blocks(T, NT)), dim3(kThreads), 0, s,
-                         (const float*)dY, (const float*)Ys, T, d, k, pos, rows, weight, (float*)dYs, dweight);
-    return hipGetLastError();
+    return over_tokens<NT>(T, [&](int64_t t0, int64_t n, dim3 grid) {
+      const float* w = weight ? weight + t0 * k : nullptr;
+      float* dw = dweight ? dweight + t0 * k : nullptr;
+      if (bf16)
+        hipLaunchKernelGGL((k_expert_combine_bwd<bf16_t, NT, KS>), grid, dim3(kThreads), 0, s,
+                           (const bf16_t*)dY + t0 * d, (const bf16_t*)Ys, n, d, k, pos + t0 * k, rows, w, (bf16_t*)dYs, dw);
+      else
+        hipLaunchKernelGGL((k_expert_combine_bwd<float, NT, KS>), grid, dim3(kThreads), 0, s,
+                           (const float*)dY + t0 * d, (const float*)Ys, n, d, k, pos + t0 * k, rows, w, (float*)dYs, dw);
+    });
   });
 }
 

@@ -1,0 +1,52 @@
+"""Calls whose work items pass 2^32, the most of one HIP launch: they go in several launches. The
+inputs are mostly zeros or unused, so that only the few rows that matter are made and compared."""
+import pytest
+import torch
+
+from tests.block_util import same_bits
+
+pytestmark = pytest.mark.gpu
+
+b = pytest.importorskip("paper_2603_23198_amd.binding")
+
+
+def room(nbytes):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < nbytes + (4 << 30):
+        pytest.skip(f"needs {nbytes >> 30} GiB of device memory")
+
+
+def test_expert_rows():
+    """2^24 tokens and more at a workgroup of 256 per token: six of them have a row."""
+    T, d = (1 << 24) + 5, 1032
+    room(2 * T * d)
+    at = torch.tensor([0, 70_000, (1 << 24) - 2, (1 << 24) - 1, 1 << 24, T - 1], device="cuda")
+    n = len(at)
+    expert = torch.full((T, 1), -1, dtype=torch.int32, device="cuda")
+    expert[at] = torch.tensor([[0], [1], [0], [1], [0], [1]], dtype=torch.int32, device="cuda")
+    want_pos = torch.tensor([0, 3, 1, 4, 2, 5], device="cuda")
+    rows = torch.randn((n, d), device="cuda").bfloat16()
+    wide = torch.empty((T, d), dtype=torch.bfloat16, device="cuda")
+    wide[at] = rows
+    pos, off = torch.empty_like(expert), torch.empty(3, dtype=torch.int32, device="cuda")
+    Xs = torch.full((n, d), -77, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(b.sfl_expert_workspace_size(T, 1, 2), dtype=torch.uint8, device="cuda")
+    b.sfl_expert_dispatch(expert, 2, pos, off, X=wide, Xs=Xs, workspace=ws)
+    assert off.tolist() == [0, 3, 6]
+    assert torch.equal(pos[at, 0].long(), want_pos) and int((pos >= 0).sum()) == n
+    assert same_bits(Xs[want_pos], rows)
+
+    dYs, dw = torch.full_like(Xs, -77), torch.full((T, 1), -77.0, device="cuda")
+    weight = torch.zeros((T, 1), device="cuda")
+    weight[at, 0] = torch.tensor([0.5, 2.0, -1.0, 4.0, 0.25, 1.0], device="cuda")
+    b.sfl_expert_combine_backward(wide, Xs, pos, weight, dYs=dYs, dweight=dw)
+    assert same_bits(dYs[want_pos], (rows.float() * weight[at]).bfloat16())
+    dot = rows.double().square().sum(1)  # within d / 64 + 32 fp32 roundings
+    assert ((dw[at, 0].double() - dot).abs() <= (d / 64 + 32) * 2.0 ** -24 * dot).all()
+    assert int((dw != 0).sum()) == n
+
+    wide.fill_(-77)
+    b.sfl_expert_combine(Xs, pos, wide, weight=weight)
+    assert same_bits(wide[at], (rows.float() * weight[at]).bfloat16())
+    wide[at] = 0
+    assert not any(part.any() for part in wide.split(1 << 20))
