@@ -381,20 +381,6 @@ template <typename F> hipError_t with_threads(int64_t d, int k, F f) {
   return hipErrorInvalidValue;
 }
 
-// Calls f with a first token, a number of tokens and their workgroups, for as many tokens at a time
-// as one launch takes (2^24 - 1 where each has a workgroup of its own).
-template <int NT, typename F> hipError_t over_tokens(int64_t T, F f) {
-  constexpr int per = kThreads / NT;
-  constexpr int64_t most = max_blocks(kThreads) * per;
-  for (int64_t t0 = 0; t0 < T; t0 += most) {
-    const int64_t n = std::min(T - t0, most);
-    f(t0, n, dim3((unsigned)cdiv(n, per)));
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
-}
-
 }  // namespace
 
 // The counts of as many workgroups as n slots can take, not of those that they do take (with runs of
@@ -433,7 +419,7 @@ hipError_t launch_expert_dispatch(const int32_t* expert, int64_t T, int k, int E
   if (!X || rows == 0) return hipGetLastError();
   return with_threads(d, k, [&](auto nt, auto) {
     constexpr int NT = decltype(nt)::value;
-    return over_tokens<NT>(T, [&](int64_t t0, int64_t n, dim3 grid) {
+    return over_tokens<kThreads, kThreads / NT>(T, [&](int64_t t0, int64_t n, dim3 grid) {
       if (bf16)
         hipLaunchKernelGGL((k_expert_rows<bf16_t, NT>), grid, dim3(kThreads), 0, s, (const bf16_t*)X + t0 * d, n, d, k,
                            pos + t0 * k, rows, (bf16_t*)Xs);
@@ -448,7 +434,7 @@ hipError_t launch_expert_combine(const void* Ys, int bf16, int64_t T, int64_t d,
                                  int64_t rows, const float* weight, void* Y, hipStream_t s) {
   return with_threads(d, k, [&](auto nt, auto ks) {
     constexpr int NT = decltype(nt)::value, KS = decltype(ks)::value;
-    return over_tokens<NT>(T, [&](int64_t t0, int64_t n, dim3 grid) {
+    return over_tokens<kThreads, kThreads / NT>(T, [&](int64_t t0, int64_t n, dim3 grid) {
       const float* w = weight ? weight + t0 * k : nullptr;
       if (bf16)
         hipLaunchKernelGGL((k_expert_combine<bf16_t, NT, KS>), grid, dim3(kThreads), 0, s, (const bf16_t*)Ys, n, d, k,
@@ -465,7 +451,7 @@ hipError_t launch_expert_combine_bwd(const void* dY, const void* Ys, int bf16, i
                                      hipStream_t s) {
   return with_threads(d, k, [&](auto nt, auto ks) {
     constexpr int NT = decltype(nt)::value, KS = decltype(ks)::value;
-    return over_tokens<NT>(T, [&](int64_t t0, int64_t n, dim3 grid) {
+    return over_tokens<kThreads, kThreads / NT>(T, [&](int64_t t0, int64_t n, dim3 grid) {
       const float* w = weight ? weight + t0 * k : nullptr;
       float* dw = dweight ? dweight + t0 * k : nullptr;
       if (bf16)

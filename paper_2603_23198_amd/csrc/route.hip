@@ -211,14 +211,14 @@ hipError_t launch_route_fwd(const void* logits, int bf16, int64_t T, int E, int 
                             int32_t* expert, float* weight, hipStream_t s) {
   return with_layout(E, [&](auto g, auto pl) {
     constexpr int G = decltype(g)::value, PL = decltype(pl)::value;
-    const dim3 grid((unsigned)cdiv(T, kThreads / G));
-    if (bf16)
-      hipLaunchKernelGGL((k_route_fwd<bf16_t, G, PL>), grid, dim3(kThreads), 0, s, (const bf16_t*)logits, T, E, k,
-                         normalise, scale, expert, weight);
-    else
-      hipLaunchKernelGGL((k_route_fwd<float, G, PL>), grid, dim3(kThreads), 0, s, (const float*)logits, T, E, k,
-                         normalise, scale, expert, weight);
-    return hipGetLastError();
+    return over_tokens<kThreads, kThreads / G>(T, [&](int64_t t0, int64_t n, dim3 grid) {
+      if (bf16)
+        hipLaunchKernelGGL((k_route_fwd<bf16_t, G, PL>), grid, dim3(kThreads), 0, s, (const bf16_t*)logits + t0 * E, n,
+                           E, k, normalise, scale, expert + t0 * k, weight + t0 * k);
+      else
+        hipLaunchKernelGGL((k_route_fwd<float, G, PL>), grid, dim3(kThreads), 0, s, (const float*)logits + t0 * E, n, E,
+                           k, normalise, scale, expert + t0 * k, weight + t0 * k);
+    });
   });
 }
 
@@ -226,14 +226,14 @@ hipError_t launch_route_bwd(const void* logits, int bf16, int64_t T, int E, int 
                             const int32_t* expert, const float* dweight, void* dlogits, hipStream_t s) {
   return with_layout(E, [&](auto g, auto pl) {
     constexpr int G = decltype(g)::value, PL = decltype(pl)::value;
-    const dim3 grid((unsigned)cdiv(T, kThreads / G));
-    if (bf16)
-      hipLaunchKernelGGL((k_route_bwd<bf16_t, G, PL>), grid, dim3(kThreads), 0, s, (const bf16_t*)logits, T, E, k,
-                         normalise, scale, expert, dweight, (bf16_t*)dlogits);
-    else
-      hipLaunchKernelGGL((k_route_bwd<float, G, PL>), grid, dim3(kThreads), 0, s, (const float*)logits, T, E, k,
-                         normalise, scale, expert, dweight, (float*)dlogits);
-    return hipGetLastError();
+    return over_tokens<kThreads, kThreads / G>(T, [&](int64_t t0, int64_t n, dim3 grid) {
+      if (bf16)
+        hipLaunchKernelGGL((k_route_bwd<bf16_t, G, PL>), grid, dim3(kThreads), 0, s, (const bf16_t*)logits + t0 * E, n,
+                           E, k, normalise, scale, expert + t0 * k, dweight + t0 * k, (bf16_t*)dlogits + t0 * E);
+      else
+        hipLaunchKernelGGL((k_route_bwd<float, G, PL>), grid, dim3(kThreads), 0, s, (const float*)logits + t0 * E, n, E,
+                           k, normalise, scale, expert + t0 * k, dweight + t0 * k, (float*)dlogits + t0 * E);
+    });
   });
 }
 

@@ -188,4 +188,17 @@ template <int N> __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
+// Calls f with a first token, a number of tokens and their workgroups (of THREADS threads, PER tokens
+// each), for as many tokens at a time as one launch takes: 2^24 - 1 workgroups of 256 threads.
+template <int THREADS, int PER, typename F> hipError_t over_tokens(int64_t T, F f) {
+  constexpr int64_t most = max_blocks(THREADS) * PER;
+  for (int64_t t0 = 0; t0 < T; t0 += most) {
+    const int64_t n = T - t0 < most ? T - t0 : most;
+    f(t0, n, dim3((unsigned)cdiv(n, PER)));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 }  // namespace sfl

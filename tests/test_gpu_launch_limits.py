@@ -50,3 +50,26 @@ def test_expert_rows():
     assert same_bits(wide[at], (rows.float() * weight[at]).bfloat16())
     wide[at] = 0
     assert not any(part.any() for part in wide.split(1 << 20))
+
+
+@pytest.mark.parametrize("E", [130, 300])
+def test_router(E):
+    """2^26 tokens at a wave per token, against calls of a few of them."""
+    T, k = (1 << 26) + 3, 2
+    room(2 * 2 * T * E + 4 * 4 * T * k)
+    if E == 130:
+        logits = torch.empty((T, E), dtype=torch.bfloat16, device="cuda").normal_()
+    else:  # 40 GB: the same rows again and again
+        logits = torch.randn((1 << 10, E), device="cuda").bfloat16().repeat((1 << 16) + 1, 1)[:T]
+    dweight = torch.randn((T, k), device="cuda")
+    expert, weight = torch.full((T, k), -7, dtype=torch.int32, device="cuda"), torch.empty((T, k), device="cuda")
+    dlogits = torch.full_like(logits, -77)
+    b.sfl_route_forward(logits, expert, weight)
+    b.sfl_route_backward(logits, expert, dweight, dlogits)
+    assert int((expert < 0).sum()) == 0
+    for z in (9, 1 << 25, (1 << 26) - 4, (1 << 26) - 3, 1 << 26, T):
+        s = slice(z - 9, z)
+        e, w, dl = expert[s].clone(), weight[s].clone(), dlogits[s].clone()
+        b.sfl_route_forward(logits[s], e.zero_(), w.zero_())
+        b.sfl_route_backward(logits[s], e, dweight[s], dl.zero_())
+        assert torch.equal(e, expert[s]) and same_bits(w, weight[s]) and same_bits(dl, dlogits[s])
