@@ -11,6 +11,7 @@
 #include "rows.h"
 
 #include <algorithm>
+#include <utility>
 
 namespace sfl {
 
@@ -176,58 +177,61 @@ int64_t elements(const sfl_grad_t* list, int n) {
   return total;
 }
 
-const char* target(const sfl_grad_t& g) { return (const char*)(g.dst ? g.dst : g.src); }
+// How far a pass over the list has come: so many tensors from its start (or its end) and so many
+// elements of the next one.
+struct Walk {
+  int tensor = 0;
+  int64_t elements = 0;
+};
 
-// Whether b's elements lie right behind a's, at the source and at the target (views of one bucket
-// mostly do): the two then go as one range, with fewer launches and no ragged shares.
-bool follows(const sfl_grad_t& a, const sfl_grad_t& b) {
-  const int64_t bytes = a.n * (a.dtype == SFL_BF16 ? 2 : 4);
-  return a.dtype == b.dtype && (const char*)a.src + bytes == (const char*)b.src && target(a) + bytes == target(b);
-}
-
-// Fills l with the ranges of tensors from list[i] on (from the list's end where `back`) and moves i
-// past them; returns the launch's workgroups.
-int64_t next_launch(const sfl_grad_t* list, int n, bool back, int64_t share, int* i, GradList<kListMax>* l) {
-  int begin = *i, end = *i, ranges = 0, last = -1;
-  int64_t closed = 0, open = 0;  // workgroups of the ranges before the last one, elements of that
-  for (; *i < n; ++*i) {
-    const int at = back ? n - 1 - *i : *i;
-    const int64_t len = list[at].n;
-    if (len > 0) {
-      const bool joins = last >= 0 && (back ? follows(list[at], list[last]) : follows(list[last], list[at]));
-      const int64_t c = joins ? closed : closed + cdiv(open, share), o = joins ? open + len : len;
-      if (ranges + !joins > kListMax || c + cdiv(o, share) > INT32_MAX) break;
-      ranges += !joins;
-      closed = c;
-      open = o;
-      last = at;
-    }
-    end = *i + 1;
-  }
-  if (back) {
-    const int b = n - end;
-    end = n - begin;
-    begin = b;
-  }
+// Fills l with the next ranges of the list, from its start on or from its end back, for as many
+// workgroups as one launch takes, and moves w past them; returns the launch's workgroups. Tensors
+// whose elements lie end to end at the source and at the target (views of one bucket mostly do) go
+// as one range, with fewer launches and no ragged shares.
+int64_t next_launch(const sfl_grad_t* list, int n, bool back, int64_t share, Walk* w, GradList<kListMax>* l) {
+  constexpr int64_t most = max_blocks(kThreads);
+  int64_t closed = 0;  // workgroups of the ranges before the last one
   l->count = 0;
   l->share = (int32_t)share;
-  l->first[0] = 0;
-  last = -1;
-  for (int j = begin; j < end; ++j) {
-    if (list[j].n == 0) continue;
-    if (last >= 0 && follows(list[last], list[j])) {
-      l->n[l->count - 1] += list[j].n;
-    } else {
-      const int m = l->count++;
-      l->src[m] = list[j].src;
-      l->dst[m] = (void*)target(list[j]);
-      l->n[m] = list[j].n;
-      l->bf16[m] = list[j].dtype == SFL_BF16;
+  for (; w->tensor < n; ++w->tensor, w->elements = 0) {
+    const sfl_grad_t& g = list[back ? n - 1 - w->tensor : w->tensor];
+    const bool bf16 = g.dtype == SFL_BF16;
+    const int64_t size = bf16 ? 2 : 4, rest = g.n - w->elements, len = std::min(rest, most * share);
+    if (len == 0) continue;
+    const int64_t at = (back ? rest - len : w->elements) * size;
+    const char* src = (const char*)g.src + at;
+    char* dst = (char*)(g.dst ? g.dst : const_cast<void*>(g.src)) + at;
+    int m = l->count - 1;  // the range that the elements may join
+    bool joins = false;
+    if (m >= 0 && l->bf16[m] == bf16) {
+      const int64_t by = (back ? len : -l->n[m]) * size;
+      joins = src + by == (const char*)l->src[m] && dst + by == (char*)l->dst[m];
     }
-    last = j;
-    const int m = l->count - 1;
-    l->first[m + 1] = l->first[m] + (int32_t)cdiv(l->n[m], share);
+    const int64_t behind = joins || m < 0 ? closed : closed + cdiv(l->n[m], share);
+    const int64_t total = joins ? l->n[m] + len : len;
+    if (l->count + !joins > kListMax || behind + cdiv(total, share) > most) break;
+    closed = behind;
+    if (!joins) m = l->count++;
+    if (!joins || back) {
+      l->src[m] = src;
+      l->dst[m] = dst;
+    }
+    l->n[m] = total;
+    l->bf16[m] = bf16;
+    if (len < rest) {  // the launch is full
+      w->elements += len;
+      break;
+    }
   }
+  if (back)
+    for (int i = 0, j = l->count - 1; i < j; ++i, --j) {
+      std::swap(l->src[i], l->src[j]);
+      std::swap(l->dst[i], l->dst[j]);
+      std::swap(l->n[i], l->n[j]);
+      std::swap(l->bf16[i], l->bf16[j]);
+    }
+  l->first[0] = 0;
+  for (int m = 0; m < l->count; ++m) l->first[m + 1] = l->first[m] + (int32_t)cdiv(l->n[m], share);
   return l->first[l->count];
 }
 
@@ -267,8 +271,8 @@ hipError_t launch_grad_sumsq(const sfl_grad_t* list, int n, double* sumsq, doubl
   const int64_t share = share_of(elements(list, n), kSumShare);
   int64_t done = 0;
   GradList<kListMax> l;
-  for (int i = 0; i < n;) {
-    const int64_t blocks = next_launch(list, n, false, share, &i, &l);
+  for (Walk w; w.tensor < n;) {
+    const int64_t blocks = next_launch(list, n, false, share, &w, &l);
     if (blocks)
       with_list(l, [&](const auto& a) {
         hipLaunchKernelGGL(k_grad_sumsq, dim3((unsigned)blocks), dim3(kThreads), 0, s, a, part + done);
@@ -289,8 +293,8 @@ hipError_t launch_grad_clip(const sfl_grad_t* list, int n, const double* sumsq, 
     });
     norm = nullptr;  // the first launch writes it
   };
-  for (int i = 0; i < n;) {
-    const int64_t blocks = next_launch(list, n, true, share, &i, &l);
+  for (Walk w; w.tensor < n;) {
+    const int64_t blocks = next_launch(list, n, true, share, &w, &l);
     if (blocks) launch(blocks);
   }
   if (norm) {  // nothing to scale

@@ -73,3 +73,41 @@ def test_router(E):
         b.sfl_route_forward(logits[s], e.zero_(), w.zero_())
         b.sfl_route_backward(logits[s], e, dweight[s], dl.zero_())
         assert torch.equal(e, expert[s]) and same_bits(w, weight[s]) and same_bits(dl, dlogits[s])
+
+
+def test_one_gradient():
+    """A tensor of more shares than the scaling pass has workgroups in a launch."""
+    share, n = 4096, (1 << 36) + 77
+    room(2 * n)
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    most = ((1 << 32) - 1) // 256 * share
+    at = sorted({0, 1, share, n // 2, most - 1, most, most + 1, n - most - 1, n - most, n - most + 1, n - share, n - 1})
+    for i in at:
+        g[i] = 2.0
+    grads = b.grad_list([g])
+    q = torch.empty(1, dtype=torch.float64, device="cuda")
+    norm = torch.empty(1, device="cuda")
+    b.sfl_grad_sumsq(grads, q, workspace=torch.empty(b.sfl_grad_workspace_size(grads), dtype=torch.uint8, device="cuda"))
+    assert q.item() == 4.0 * len(at)
+    b.sfl_grad_clip(grads, q, norm.copy_(q.sqrt() / 4).item(), norm)
+    assert abs(norm.item() - q.sqrt().item()) <= 2.0 ** -23 * norm.item()
+    assert [g[i].item() for i in at] == [0.5] * len(at)
+    for i in at:
+        g[i] = 0
+    assert not any(part.any() for part in g.split(1 << 31))
+
+
+def test_many_large_gradients():
+    """Ranges whose shares pass a launch of the sum together (one tensor, listed again and again; an
+    allowed norm above theirs leaves it as it is)."""
+    n, times = (1 << 31) + 9, 70
+    room(2 * n)
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g[0], g[n // 3], g[n - 1] = 1.0, 2.0, 2.0
+    grads = b.grad_list([g] * times)
+    q, norm = torch.empty(1, dtype=torch.float64, device="cuda"), torch.empty(1, device="cuda")
+    b.sfl_grad_sumsq(grads, q, workspace=torch.empty(b.sfl_grad_workspace_size(grads), dtype=torch.uint8, device="cuda"))
+    assert q.item() == 9.0 * times
+    b.sfl_grad_clip(grads, q, 1e6, norm)
+    assert abs(norm.item() - (9.0 * times) ** 0.5) <= 2.0 ** -23 * norm.item()
+    assert [g[i].item() for i in (0, n // 3, n - 1)] == [1.0, 2.0, 2.0]
