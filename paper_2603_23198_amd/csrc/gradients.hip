@@ -138,8 +138,19 @@ __global__ __launch_bounds__(kSumThreads) void k_grad_sum(const double* __restri
   if (threadIdx.x == 0) *sumsq = s;
 }
 
-template <typename V> __device__ __forceinline__ void share_scale(const V* p, V* q, int n, float by) {
-  if (p == q && by == 1.f) return;
+// A clipping coefficient, by 2^exp. exp is 0 where by alone is a normal fp32 number: a subnormal one has
+// fewer bits than the gradients (max_norm = 1e-3 of a norm of 3e38: 1e-4 off), and a smaller one is 0.
+struct Scale {
+  float by;
+  int exp;
+  __device__ __forceinline__ Scale(double c) : by((float)c), exp(0) {
+    if (c > 0 && c < 0x1p-126) by = (float)frexp(c, &exp);
+  }
+  __device__ __forceinline__ float operator()(float g) const { return ldexpf(g * by, exp); }
+};
+
+template <typename V> __device__ __forceinline__ void share_scale(const V* p, V* q, int n, const Scale& scale) {
+  if (p == q && scale.by == 1.f && scale.exp == 0) return;
   using S = Step<V>;
   constexpr int kSteps = kScaleShare / S::kStep;
   const int c = threadIdx.x * S::kElems;
@@ -149,7 +160,7 @@ template <typename V> __device__ __forceinline__ void share_scale(const V* p, V*
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
 #pragma unroll
-    for (int e = 0; e < S::kElems; ++e) VT<V>::store(v[i].e, e, VT<V>::load(v[i].e, e) * by);
+    for (int e = 0; e < S::kElems; ++e) VT<V>::store(v[i].e, e, scale(VT<V>::load(v[i].e, e)));
     v[i].store(q, c + i * S::kStep, n);
   }
 }
@@ -160,7 +171,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_scale(GradList<MAX> l, const 
   const double nrm = sqrt(*sumsq);
   const float shown = (float)nrm;  // infinite where fp32 cannot hold it, and then nothing is scaled
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = shown;
-  const float by = nrm > (double)max_norm && shown < INFINITY ? (float)((double)max_norm / nrm) : 1.f;
+  const Scale by(nrm > (double)max_norm && shown < INFINITY ? (double)max_norm / nrm : 1.0);
   if (l.count == 0) return;
   const int b = gridDim.x - 1 - blockIdx.x, i = range_of(l, b);
   const int64_t at = (int64_t)(b - l.first[i]) * l.share;

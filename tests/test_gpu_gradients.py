@@ -157,3 +157,10 @@ def test_more_elements_than_32_bits():
     assert q.item() == 49.0
     b.sfl_grad_clip(grads, q, 3.5)
     assert [g[i].item() for i in (0, n // 2, n - 1)] == [1.0, 1.5, 3.0] and g[1].item() == 0
+
+
+@pytest.mark.parametrize("std,max_norm", [(1e36, 1e-3), (1e36, 1.0), (1e18, 1e-30), (3e-5, 1e-25), (1e30, 1e-12)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_coefficients_below_the_fp32_range(std, max_norm, in_place):
+    """max_norm / norm may be subnormal or zero in fp32 where the scaled gradients are ordinary numbers."""
+    check([5000, 333], ["f32", "bf16"], max_norm, std=std, in_place=in_place)
