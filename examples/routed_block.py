@@ -144,10 +144,13 @@ class RoutedStack:
         return dX
 
     def step(self, lr, max_norm):
-        """Clips the gradients by their global norm and applies them; returns the norm (device)."""
+        """Clips the gradients by their global norm and applies them; returns the norm (device). Where
+        it is not finite, nothing was scaled and the step is left out."""
         ws = self._space("clip", b.sfl_grad_workspace_size(self.clip_list))
         b.sfl_grad_sumsq(self.clip_list, self.sumsq, workspace=ws)
         b.sfl_grad_clip(self.clip_list, self.sumsq, max_norm, self.norm)
+        if not self.norm.isfinite().item():
+            return self.norm
         for blk, g, half in zip(self.blocks, self.grads, self.halves):
             for n in blk:
                 blk[n].sub_(g[n], alpha=lr)

@@ -130,3 +130,20 @@ def test_under_graph_capture():
         torch.cuda.synchronize()
         for a, c in zip(got, outs):
             assert torch.equal(a.view(torch.uint8), c.view(torch.uint8))
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_a_step_whose_norm_is_not_finite_changes_nothing(bad):
+    m = rb.RoutedStack(1, 512, 256, 4, 2)
+    for g in m.all_grads():
+        g.fill_(1.0)
+    m.grads[0]["W_up"][1, 3, 7] = bad
+    params = [p for blk in m.blocks for p in blk.values()] + [m.w_out]
+    halves = [h for half in m.halves for h in half.values()]
+    before = [t.clone() for t in params + halves]
+    norm = m.step(0.1, 1.0)
+    assert not norm.isfinite().item()
+    assert all(torch.equal(a, t) for a, t in zip(before, params + halves))
+    m.grads[0]["W_up"].fill_(1.0)
+    assert m.step(0.1, 1.0).isfinite().item()
+    assert not any(torch.equal(a, t) for a, t in zip(before, params))
