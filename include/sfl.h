@@ -563,7 +563,7 @@ sfl_status_t sfl_route_backward(const void* logits, sfl_dtype_t dtype, int64_t T
 /* Tokens to their experts. Slot (t, j), the j-th choice of token t, gets a row of the expert order:
  * rows are sorted by expert, an expert's rows by slot.
  *  expert  [T][k] int32; a value outside [0, E) names no expert (the slot gets no row)
- *  pos     [T][k] int32: the slot's row, or -1
+ *  pos     [T][k] int32: the slot's row, or -1; does not overlap expert
  *  offsets [E + 1] int32: the first row of each expert; offsets[E] is the number of rows
  *  X, Xs   rows [T][d] and their copies in expert order, Xs[pos[t][j]] = X[t], Xs [rows][d]; both
  *          NULL to make the order alone. A row beyond `rows` is not written, rows from offsets[E]

@@ -13,7 +13,7 @@
 // token and about 10 to 30 operations are done per element. So a row is read once and held in
 // registers between its sums and its outputs, eight elements per thread and chunk. Measured, passes
 // back to back: forward of 8192 x 4096 bf16 50 us (5.3 TB/s), backward of 16384 x 4096 bf16 with all
-// parameter gradients 147 us (5.5 TB/s); a 1 GiB copy reaches 5.2. The simplest kernels (a workgroup
+// parameter gradients 147 to 149 us (5.4 TB/s); a 1 GiB copy reaches 5.2. The simplest kernels (a workgroup
 // of 256 threads per row, rows read again for every sum) took 186 and 1927.
 #include "block.h"
 #include "rows.h"
@@ -155,7 +155,8 @@ __global__ __launch_bounds__(Rows<NT>::kThreads) void k_norm_fwd(NormParams p) {
 // HOLD: the row, the weights and the parameter sums stay in registers; else (wide rows) the row and
 // the weights are read again, from L2, for the outputs, and the sums are kept in LDS.
 // A bf16 row's loads go out while the row before it is still being summed (16 registers; fp32 rows
-// have twice the bytes in flight without).
+// have twice the bytes in flight without). Above 512 columns that takes the bf16 kernel past its 128
+// registers: four go to scratch, and so do eleven of the fp32 kernel above 4096 columns.
 template <typename V> struct BwdRow {
   Vec8<V> X, Y, G, N;  // X_out, Y, dX_out, dN
   __device__ __forceinline__ void load(const NormBwdParams& p, int64_t base, Cols c, int d) {
@@ -348,7 +349,9 @@ __global__ __launch_bounds__(kSumThreads) void k_norm_param_sums(NormBwdParams p
 }
 
 // Calls f with NT, CH and the threads of a workgroup for a width: one chunk per thread up to 8192
-// columns, then two.
+// columns, then two (row tensors of 2^26 bytes, d = 16384: forward 56 us bf16 and 67 fp32, of which 20
+// registers go to scratch; backward 142 and 134; just above 8192 columns, with nearly half the lanes'
+// second chunks empty, 70 and 76, and 237 and 152).
 template <typename F> hipError_t with_layout(int64_t d, F f) {
   using std::integral_constant;
   const int64_t n = cdiv(d, kVec);
@@ -363,10 +366,12 @@ template <typename F> hipError_t with_layout(int64_t d, F f) {
 }  // namespace
 
 // Workgroups of the backward. The fewer there are, the more rows each adds up before it leaves its
-// sums, so a CU gets the twelve waves (eight of fp32) that keep the memory busy with full loads, or
-// all sixteen (twelve) that its registers hold where rows leave lanes idle or are not whole in units
-// (rows of 2^26 bytes in all, bf16 d = 4096: 81 us with twelve waves, 89 with sixteen; d = 640: 139
-// and 119; fp32 d = 2048: 81 with eight, 90 with twelve).
+// sums, so a CU gets as many as fit into twelve waves (eight of fp32), and one at least, which keep the
+// memory busy with full loads, or into all sixteen (twelve) that its registers hold where rows leave
+// lanes idle or are not whole in units. Row tensors of 2^26 bytes, all gradients: bf16 d = 2048 (three
+// workgroups of four waves) 81 us, four of them 88; d = 4096 (one of eight waves) 82, two 83 (147 and 154
+// at twice the rows); d = 640 (sixteen waves) 98, twelve 114; fp32 d = 2048 (eight) 79, twelve 82; d = 640
+// (twelve) 86, eight 95.
 static int64_t bwd_blocks(int64_t T, int64_t d, int bf16) {
   int64_t blocks = 0;
   (void)with_layout(d, [&](auto nt, auto, int threads) {

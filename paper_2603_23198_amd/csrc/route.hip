@@ -5,7 +5,9 @@
 // dl_i = p_i (up_i - sum_j s_j G_j), p over the chosen (normalise) or all available experts,
 // up_i = G_j for a chosen expert and 0 for another.
 //
-// The data is small (16384 x 64 logits are 4 MB); the instructions of the k rounds bound it. A token
+// The data is small (16384 x 64 logits are 4 MB), and the k rounds cost more than it: in a captured
+// graph 65536 tokens of 64 fp32 logits take 6.6 us for k = 1 and 0.8 for every further choice, 16384 take
+// 3.1 and 0.27 (at k = 8, 5.0 in all, 440 vector instructions a wave, which alone take 3 us). A token
 // therefore takes a group of G lanes with PL experts each, PL = 4 for up to 256 experts: a round's
 // exchange between lanes (two instructions per halving) then serves several tokens of a wave, and
 // what a lane does for its own PL experts costs less than more lanes would. 16384 tokens, 8 of 64,
