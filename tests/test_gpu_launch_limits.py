@@ -10,6 +10,13 @@ pytestmark = pytest.mark.gpu
 b = pytest.importorskip("paper_2603_23198_amd.binding")
 
 
+@pytest.fixture(autouse=True)
+def released():
+    """The next test finds the memory free again."""
+    yield
+    torch.cuda.empty_cache()
+
+
 def room(nbytes):
     torch.cuda.empty_cache()
     if torch.cuda.mem_get_info()[0] < nbytes + (4 << 30):
