@@ -624,6 +624,200 @@ sfl_status_t sfl_grad_workspace_size(const sfl_grad_t* list, int32_t n, size_t* 
 sfl_status_t sfl_grad_clip(const sfl_grad_t* list, int32_t n, const double* sumsq, float max_norm, float* norm,
                            sfl_stream_t stream);
 
+/* ---- Many routed experts in 8 bits -------------------------------------------------------
+ * What a model of many routed experts has beside the operators above: a router with groups of
+ * experts, the experts' matrices and rows in 8-bit floating point with the products between them, and
+ * the optimiser's step. The conventions above hold. The experts' row counts stay on the device
+ * (sfl_expert_dispatch's offsets), so a block can be captured into a graph whole. */
+
+enum {
+  SFL_SCORE_SIGMOID = 0, /* of each logit by itself */
+  SFL_SCORE_SOFTMAX = 1  /* over the token's available experts */
+};
+
+/* Router with groups. An expert is available to a token where its logit l is neither -inf nor NaN.
+ *   s_e = score of l_e; c_e = s_e + bias_e, formed in 64 bits and rounded to fp32; an expert can be
+ *   chosen where it is available and c_e is neither -inf nor NaN
+ *   The experts are `groups` runs of E / groups. With more than one, a group's worth is the sum (in
+ *   fp32) of its group_top largest c (of fewer where it has fewer; a group without any is not
+ *   taken), and the experts of the group_k worthiest groups can be chosen.
+ *   expert [T][k] int32: those with the k largest c, in that order; -1 where fewer can be chosen
+ *   weight [T][k] fp32: scale s_j / (sum of s over the chosen experts) with normalise = 1, else
+ *          scale s_j; 0 where expert is -1. Where the scores underflow, their quotients are still those
+ *          of the reals.
+ * Equal c or worths (+0 and -0 are) go by ascending index. Logits of +inf have a sigmoid of one and
+ * share a softmax evenly.
+ *  logits [T][E] dtype; bias [E] fp32 or NULL for zeros (it has no part in the weights and no
+ *          gradient: it is moved by the experts' loads)
+ * 1 <= E <= 1024, E divisible by groups, 1 <= group_k <= groups, group_top 1 or 2,
+ * 1 <= k <= min(64, group_k E / groups). Errors: SFL_E_ARG for bad sizes, an unknown score or flag or
+ * a NULL buffer (T > 0); SFL_E_UNSUPPORTED for E > 1024, k > 64 or T > 2^31 - 1. */
+typedef struct {
+  sfl_dtype_t dtype;
+  int32_t score;
+  int64_t T;
+  int32_t E, k;
+  int32_t groups, group_k, group_top;
+  int32_t normalise;
+  float scale;
+  const void* logits;
+  const float* bias;
+  int32_t* expert;
+  float* weight;
+} sfl_route_groups_args_t;
+sfl_status_t sfl_route_groups_forward(const sfl_route_groups_args_t* args, sfl_stream_t stream);
+
+/* Gradient of the weights with respect to the logits: dlogits [T][E] (dtype, overwritten) from
+ * dweight [T][k] fp32 and the forward's expert. The choice is taken as constant; dweight is not read
+ * where expert is outside [0, E), and the logit of an expert that is not available gets 0. Errors as
+ * above. */
+typedef struct {
+  sfl_dtype_t dtype;
+  int32_t score;
+  int64_t T;
+  int32_t E, k;
+  int32_t normalise;
+  float scale;
+  const void* logits;
+  const int32_t* expert;
+  const float* dweight;
+  void* dlogits;
+} sfl_route_groups_bwd_args_t;
+sfl_status_t sfl_route_groups_backward(const sfl_route_groups_bwd_args_t* args, sfl_stream_t stream);
+
+/* Numbers in 8 bits: e4m3 codes (4 exponent and 3 mantissa bits, no infinity, largest 448) and a scale
+ * for each block of 128, a byte b for 2^(b - 127). A block's scale is the smallest such power, from
+ * 2^-127 on, by which the largest magnitude of its finite elements comes down to 448 (2^0 for a block
+ * of zeros); its codes are the nearest e4m3 numbers to the scaled elements, halves to even. An element
+ * that is not finite becomes NaN, and no other does. Scales by powers of two lose nothing that e4m3
+ * holds, and the matrix cores apply them inside the product.
+ *  Rows     X [T][d]: codes Q [T][dq], dq = d up to a multiple of 128, zeros behind d; scales S
+ *           [T][sq], sq = dq / 128 up to a multiple of 4, 127 behind the blocks
+ *  Columns  blocks along the tokens, for products that sum over them: codes Qt [d][columns], scales
+ *           St [d][columns / 128]. The tokens are E runs, run e of X's rows offsets[e] to
+ *           offsets[e + 1]; each takes whole blocks, one run behind the other, with zeros behind its
+ *           last token. sfl_quant_columns gives `columns` for any E runs of T tokens in all, a multiple
+ *           of 512; what lies behind the last run is left as it is.
+ * Code buffers are 16-byte, scale buffers 4-byte aligned. */
+
+/* Arguments of sfl_quant_rows.
+ *  X        [T][d] dtype
+ *  where    [T][d] dtype or NULL: elements where it is not above zero are taken as zero (the rows of
+ *           a ReLU before it, or their gradient). May be X.
+ *  Q, S     rows, both or neither
+ *  Qt, St   columns, both or neither, of `columns` (a multiple of 512, at least sfl_quant_columns)
+ *  offsets  [E + 1] int32, ascending from 0 or above to at most T, NULL for one run of all rows (E =
+ *           1). Tokens in no run are in no column, and their rows of Q and S are left as they are.
+ *           Offsets that descend or pass T give codes without meaning (never an access out of bounds).
+ * Errors: SFL_E_ARG for bad sizes, NULL or misaligned buffers, neither rows nor columns; SFL_E_UNSUPPORTED for
+ * E > 1024, T > 2^31 - 1 - 128 E or d > 2^20. */
+typedef struct {
+  sfl_dtype_t dtype;
+  int32_t E;
+  int64_t T, d, columns;
+  const void* X;
+  const void* where;
+  const int32_t* offsets;
+  uint8_t* Q;
+  uint8_t* S;
+  uint8_t* Qt;
+  uint8_t* St;
+} sfl_quant_args_t;
+sfl_status_t sfl_quant_rows(const sfl_quant_args_t* args, sfl_stream_t stream);
+/* *columns (host): of Qt for T tokens of E experts. Never less for more of either. */
+sfl_status_t sfl_quant_columns(int64_t T, int32_t E, int64_t* columns);
+
+/* E weight matrices W [E][R][C] (dtype) with a scale for each 128 x 128, which serves both layouts:
+ *  Q   [E][R][Cq] codes, S  [E][R up to 128s / 128][Cq / 128 up to 4s] scales; both or neither
+ *  Qt  [E][C][Rq] codes of the transposes, St [E][C up to 128s / 128][Rq / 128 up to 4s]; both or neither
+ * Errors as above; SFL_E_UNSUPPORTED for R or C > 2^20. */
+sfl_status_t sfl_quant_weights(const void* W, sfl_dtype_t dtype, int64_t E, int64_t R, int64_t C, uint8_t* Q,
+                               uint8_t* S, uint8_t* Qt, uint8_t* St, sfl_stream_t stream);
+
+/* Rows of the experts in order times their experts' weights: for e < E, offsets[e] <= t < offsets[e + 1],
+ *   Y[t][n] = sum_k x[t][k] w[e][n][k]
+ * in fp32 on the matrix cores, rounded once to dtype.
+ *  Q, S     x: rows as sfl_quant_rows has them, [rows][K] and their scales, K a multiple of 128
+ *  W, Ws    w: E matrices [N][K] as sfl_quant_weights has them (Q and S for X W^T, Qt and St for the
+ *           gradient of the rows, dY W)
+ *  offsets  [E + 1] int32 as above, NULL for one expert of all rows
+ *  Y        [rows][N] dtype (F32 or BF16); rows of no expert are left as they are
+ * Results below the normal fp32 numbers may be zero. The sums' order depends on the sizes and not on the
+ * rows' places. Errors: SFL_E_ARG for bad sizes, NULL or misaligned buffers; SFL_E_UNSUPPORTED for
+ * E > 1024, rows or N > 2^31 - 1 - 128 E or K > 2^20. */
+sfl_status_t sfl_quant_product(const uint8_t* Q, const uint8_t* S, int64_t rows, int64_t K, const uint8_t* W,
+                               const uint8_t* Ws, int32_t E, int64_t N, const int32_t* offsets, sfl_dtype_t dtype,
+                               void* Y, sfl_stream_t stream);
+
+/* Gradients of the weights: for every e, dW[e][n][k] = sum over the tokens t of run e of y[t][n] x[t][k].
+ *  Yt, Ys, Xt, Xs  y and x: columns as sfl_quant_rows has them, [N][columns] and [K][columns], of the same
+ *           offsets
+ *  dW       [E][N][K] dtype, overwritten; zeros for an expert without tokens
+ *  rows     the tokens that the columns hold, or more (offsets are held to it), at most `columns`
+ * N and K need not be multiples of anything. Errors as above (N, K <= 2^20). */
+sfl_status_t sfl_quant_product_weights(const uint8_t* Yt, const uint8_t* Ys, int64_t N, const uint8_t* Xt,
+                                       const uint8_t* Xs, int64_t K, int64_t rows, int64_t columns,
+                                       const int32_t* offsets, int32_t E, sfl_dtype_t dtype, void* dW,
+                                       sfl_stream_t stream);
+
+enum {
+  SFL_MOMENTS_F32 = 0,
+  SFL_MOMENTS_8BIT = 1 /* e4m3 codes and a scale byte for each 128 elements; of the second moment the root */
+};
+
+/* One tensor of a list for sfl_adamw_step (the list is host memory, read during the call only).
+ *  param    n elements of param_dtype, updated in place
+ *  grad     n elements of grad_dtype
+ *  half     n bf16: the new parameters rounded to bf16 (for fp32 ones), or NULL
+ *  m, v     moments: n fp32, or n codes each with scales of ceil(n / 128) bytes in m_scale and v_scale;
+ *           updated in place. All zeros (scales of any value) before the first step.
+ * No tensor of the list overlaps another. */
+typedef struct {
+  void* param;
+  const void* grad;
+  void* half;
+  void* m;
+  void* v;
+  uint8_t* m_scale;
+  uint8_t* v_scale;
+  int64_t n;
+  float weight_decay;
+  int32_t param_dtype; /* sfl_dtype_t */
+  int32_t grad_dtype;  /* sfl_dtype_t */
+  int32_t moments;     /* SFL_MOMENTS_* */
+} sfl_adamw_t;
+
+/* One step of AdamW (Loshchilov and Hutter 2019) over the list, with t = *step:
+ *   g = c grad; m <- beta1 m + (1 - beta1) g; v <- beta2 v + (1 - beta2) g^2
+ *   param <- param - lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay param)
+ * in fp32. The update uses the new moments before they are held in 8 bits.
+ *  step     device int64 [1], the number of this step, from 1 on (a smaller one counts as 1)
+ *  lr_scale device fp32 [1] by which lr is multiplied, or NULL
+ *  sumsq    device fp64 [1], sfl_grad_sumsq of all gradients, or NULL for c = 1: c as in sfl_grad_clip. Where
+ *           the norm is not finite, no parameter and no moment changes.
+ *  norm     device fp32 [1], sqrt(*sumsq), or NULL (needs sumsq)
+ *  seed     of the noise that 8-bit moments are rounded with
+ * A moment in 8 bits is rounded to one of its two neighbours, the nearer one more often, so that small
+ * changes of slow averages are kept on average: with h the 32 bits of mix(mix(K + hi) ^ lo), K =
+ * mix(t + mix(seed)), mix being MurmurHash3's 32-bit finaliser and hi, lo the halves of the element's place in
+ * the list (every tensor counted as whole blocks of 128), the lower 16 bits are added below the last bit that
+ * m keeps and the upper 16 below that of sqrt(v), and what is below is cut off. A root above zero never becomes
+ * zero. Moments that are not finite are held as NaN, and no others.
+ * Errors: SFL_E_ARG for n < 0, a NULL list (n > 0), cfg or step, a NULL buffer of a tensor with elements, scales
+ * missing or given for fp32 moments, an unknown type, a half of bf16 parameters, betas outside [0, 1), eps not
+ * above 0, lr, weight_decay or max_norm negative or NaN, norm without sumsq. */
+typedef struct {
+  double lr, beta1, beta2, eps; /* 1 - beta is formed in 64 bits */
+  double max_norm;              /* not read without sumsq */
+  uint32_t seed;
+  uint32_t reserved;
+  const int64_t* step;
+  const float* lr_scale;
+  const double* sumsq;
+  float* norm;
+} sfl_adamw_cfg_t;
+sfl_status_t sfl_adamw_step(const sfl_adamw_t* list, int32_t n, const sfl_adamw_cfg_t* cfg, sfl_stream_t stream);
+
 /* Measurement utility (no step of the layer uses it): the bandwidth ceilings that the
  * kernels' rates are compared against, on the machine at hand.
  *  dst != NULL: copies bytes (rounded down to 16) from src to dst, reps times (the HBM copy

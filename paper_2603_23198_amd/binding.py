@@ -55,7 +55,9 @@ EXPORTED = ["sfl_status_string", "sfl_version", "sfl_twell_buffer_sizes", "sfl_p
             "sfl_down_projection_rowwise", "sfl_forward_workspace_size", "sfl_backward_workspace_size",
             "sfl_norm_forward", "sfl_norm_backward", "sfl_norm_workspace_size", "sfl_route_forward",
             "sfl_route_backward", "sfl_expert_dispatch", "sfl_expert_workspace_size", "sfl_expert_combine",
-            "sfl_expert_combine_backward", "sfl_grad_sumsq", "sfl_grad_workspace_size", "sfl_grad_clip"]
+            "sfl_expert_combine_backward", "sfl_grad_sumsq", "sfl_grad_workspace_size", "sfl_grad_clip",
+            "sfl_route_groups_forward", "sfl_route_groups_backward", "sfl_quant_rows", "sfl_quant_columns",
+            "sfl_quant_weights", "sfl_quant_product", "sfl_quant_product_weights", "sfl_adamw_step"]
 
 
 class SflError(RuntimeError):
@@ -125,6 +127,41 @@ class Grad(Structure):
     _fields_ = [("src", c_void_p), ("dst", c_void_p), ("n", c_int64), ("dtype", c_int32), ("reserved", c_int32)]
 
 
+SFL_SCORE_SIGMOID, SFL_SCORE_SOFTMAX = 0, 1
+SFL_MOMENTS_F32, SFL_MOMENTS_8BIT = 0, 1
+
+
+class RouteGroupsArgs(Structure):
+    _fields_ = [("dtype", c_int), ("score", c_int32), ("T", c_int64), ("E", c_int32), ("k", c_int32),
+                ("groups", c_int32), ("group_k", c_int32), ("group_top", c_int32), ("normalise", c_int32),
+                ("scale", ctypes.c_float), ("logits", c_void_p), ("bias", c_void_p), ("expert", c_void_p),
+                ("weight", c_void_p)]
+
+
+class RouteGroupsBwdArgs(Structure):
+    _fields_ = [("dtype", c_int), ("score", c_int32), ("T", c_int64), ("E", c_int32), ("k", c_int32),
+                ("normalise", c_int32), ("scale", ctypes.c_float), ("logits", c_void_p), ("expert", c_void_p),
+                ("dweight", c_void_p), ("dlogits", c_void_p)]
+
+
+class QuantArgs(Structure):
+    _fields_ = [("dtype", c_int), ("E", c_int32), ("T", c_int64), ("d", c_int64), ("columns", c_int64),
+                ("X", c_void_p), ("where", c_void_p), ("offsets", c_void_p), ("Q", c_void_p), ("S", c_void_p),
+                ("Qt", c_void_p), ("St", c_void_p)]
+
+
+class Adamw(Structure):
+    _fields_ = [("param", c_void_p), ("grad", c_void_p), ("half", c_void_p), ("m", c_void_p), ("v", c_void_p),
+                ("m_scale", c_void_p), ("v_scale", c_void_p), ("n", c_int64), ("weight_decay", ctypes.c_float),
+                ("param_dtype", c_int32), ("grad_dtype", c_int32), ("moments", c_int32)]
+
+
+class AdamwCfg(Structure):
+    _fields_ = [("lr", c_double), ("beta1", c_double), ("beta2", c_double), ("eps", c_double),
+                ("max_norm", c_double), ("seed", ctypes.c_uint32), ("reserved", ctypes.c_uint32),
+                ("step", c_void_p), ("lr_scale", c_void_p), ("sumsq", c_void_p), ("norm", c_void_p)]
+
+
 _lib.sfl_status_string.restype = c_char_p
 _lib.sfl_status_string.argtypes = [c_int]
 _lib.sfl_version.restype = c_char_p
@@ -163,6 +200,17 @@ _lib.sfl_expert_combine_backward.argtypes = [c_void_p, c_void_p, c_int, c_int64,
 _lib.sfl_grad_sumsq.argtypes = [POINTER(Grad), c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
 _lib.sfl_grad_workspace_size.argtypes = [POINTER(Grad), c_int32, POINTER(c_size_t)]
 _lib.sfl_grad_clip.argtypes = [POINTER(Grad), c_int32, c_void_p, ctypes.c_float, c_void_p, c_void_p]
+_lib.sfl_route_groups_forward.argtypes = [POINTER(RouteGroupsArgs), c_void_p]
+_lib.sfl_route_groups_backward.argtypes = [POINTER(RouteGroupsBwdArgs), c_void_p]
+_lib.sfl_quant_rows.argtypes = [POINTER(QuantArgs), c_void_p]
+_lib.sfl_quant_columns.argtypes = [c_int64, c_int32, POINTER(c_int64)]
+_lib.sfl_quant_weights.argtypes = [c_void_p, c_int, c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p,
+                                   c_void_p]
+_lib.sfl_quant_product.argtypes = [c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_int32, c_int64, c_void_p,
+                                   c_int, c_void_p, c_void_p]
+_lib.sfl_quant_product_weights.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_int64, c_int64,
+                                           c_void_p, c_int32, c_int, c_void_p, c_void_p]
+_lib.sfl_adamw_step.argtypes = [POINTER(Adamw), c_int32, POINTER(AdamwCfg), c_void_p]
 for _n in EXPORTED[2:]:
     getattr(_lib, _n).restype = c_int
 
@@ -403,11 +451,11 @@ def sfl_transpose(inp, out, stream=None):
 # ---- around the layer: norms, router, experts, gradient clipping ----
 # These take the tensors themselves, so shapes, types and contiguity are checked here.
 # Device pointer of a contiguous device tensor of n elements of a type (SFL_F32, SFL_BF16 or one of
-# the two below), in rows of so many where a fourth argument says so; None for None; ValueError for
+# those below), in rows of so many where a fourth argument says so; None for None; ValueError for
 # any other.
 _buf = _marshal.ptr
 _space = _marshal.space  # (device pointer, bytes) of a contiguous device tensor, or (None, 0) for None
-_F32, _I32, _F64 = SFL_F32, 2, 3
+_F32, _BF16, _I32, _F64, _F8, _U8, _I64 = SFL_F32, SFL_BF16, 2, 3, 4, 5, 6
 
 
 def sfl_norm_forward(X, Y=None, *, X_out=None, N=None, norms=SFL_NORM_PRE | SFL_NORM_POST, w_pre=None, w_post=None,
@@ -520,6 +568,127 @@ def sfl_grad_sumsq(grads, sumsq, *, workspace=None, stream=None):
 def sfl_grad_clip(grads, sumsq, max_norm, norm=None, *, stream=None):
     _check("sfl_grad_clip", _lib.sfl_grad_clip(grads, len(grads), _buf(sumsq, _F64, 1), max_norm,
                                                _buf(norm, _F32, 1), _stream(stream)))
+
+
+# ---- many routed experts in 8 bits: router with groups, quantisation, products, AdamW ----
+_SCORES = {"sigmoid": SFL_SCORE_SIGMOID, "softmax": SFL_SCORE_SOFTMAX}
+
+
+def _up(n, m):
+    return -(-n // m) * m
+
+
+def _score(score):
+    code = _SCORES.get(score)
+    if code is None:
+        raise ValueError(f"unknown score {score!r}: 'sigmoid' or 'softmax'")
+    return code
+
+
+def sfl_route_groups_forward(logits, expert, weight, *, bias=None, score="sigmoid", groups=1, group_k=1, group_top=1,
+                             normalise=True, scale=1.0, stream=None):
+    (T, E), k, dt = logits.shape, expert.shape[1], dtype_code(logits.dtype)
+    a = RouteGroupsArgs(dt, _score(score), T, E, k, groups, group_k, group_top, 1 if normalise else 0, scale,
+                        _buf(logits, dt, T * E, E), _buf(bias, _F32, E), _buf(expert, _I32, T * k, k),
+                        _buf(weight, _F32, T * k, k))
+    _check("sfl_route_groups_forward", _lib.sfl_route_groups_forward(a, _stream(stream)))
+
+
+def sfl_route_groups_backward(logits, expert, dweight, dlogits, *, score="sigmoid", normalise=True, scale=1.0,
+                              stream=None):
+    (T, E), k, dt = logits.shape, expert.shape[1], dtype_code(logits.dtype)
+    a = RouteGroupsBwdArgs(dt, _score(score), T, E, k, 1 if normalise else 0, scale, _buf(logits, dt, T * E, E),
+                           _buf(expert, _I32, T * k, k), _buf(dweight, _F32, T * k, k), _buf(dlogits, dt, T * E, E))
+    _check("sfl_route_groups_backward", _lib.sfl_route_groups_backward(a, _stream(stream)))
+
+
+def sfl_quant_columns(T, E=1):
+    out = c_int64(0)
+    _check("sfl_quant_columns", _lib.sfl_quant_columns(T, E, out))
+    return out.value
+
+
+def _codes(Q, S, rows, width, scale_rows):
+    """Pointers of codes of so many rows and bytes a row, and of their scales."""
+    per = _up(width // 128, 4)
+    return _buf(Q, _F8, rows * width, width), _buf(S, _U8, scale_rows * per, per)
+
+
+def sfl_quant_rows(X, Q=None, S=None, *, Qt=None, St=None, where=None, offsets=None, stream=None):
+    (T, d), dt = X.shape, dtype_code(X.dtype)
+    E = 1 if offsets is None else offsets.numel() - 1
+    columns = 0 if Qt is None else Qt.shape[1]
+    a = QuantArgs(dt, E, T, d, columns, _buf(X, dt, T * d, d), _buf(where, dt, T * d, d), _buf(offsets, _I32, E + 1),
+                  *_codes(Q, S, T, _up(d, 128), T), *_codes(Qt, St, d, columns, d))
+    _check("sfl_quant_rows", _lib.sfl_quant_rows(a, _stream(stream)))
+
+
+def sfl_quant_weights(W, Q=None, S=None, *, Qt=None, St=None, stream=None):
+    R, C = W.shape[-2:]
+    E, dt = W.shape[0] if W.dim() == 3 else 1, dtype_code(W.dtype)
+    r, c = _up(R, 128), _up(C, 128)
+    _check("sfl_quant_weights",
+           _lib.sfl_quant_weights(_buf(W, dt, E * R * C, C), dt, E, R, C, *_codes(Q, S, E * R, c, E * (r // 128)),
+                                  *_codes(Qt, St, E * C, r, E * (c // 128)), _stream(stream)))
+
+
+def sfl_quant_product(Q, S, W, Ws, Y, *, offsets=None, stream=None):
+    (rows, K), N, dt = Q.shape, W.shape[-2], dtype_code(Y.dtype)
+    E = W.shape[0] if W.dim() == 3 else 1
+    if offsets is not None and offsets.numel() != E + 1:
+        raise ValueError(f"offsets of {E} experts are {E + 1}, got {offsets.numel()}")
+    q, s = _codes(Q, S, rows, K, rows)
+    w, ws = _codes(W, Ws, E * N, K, E * (_up(N, 128) // 128))
+    _check("sfl_quant_product",
+           _lib.sfl_quant_product(q, s, rows, K, w, ws, E, N, _buf(offsets, _I32, E + 1), dt,
+                                  _buf(Y, dt, rows * N, N), _stream(stream)))
+
+
+def sfl_quant_product_weights(Yt, Ys, Xt, Xs, dW, *, rows=None, offsets=None, stream=None):
+    """rows: the tokens of the one run without offsets (with them, they say how many there are)."""
+    (N, columns), K, dt = Yt.shape, Xt.shape[0], dtype_code(dW.dtype)
+    E = 1 if offsets is None else offsets.numel() - 1
+    if rows is None:
+        if offsets is None:
+            raise ValueError("sfl_quant_product_weights: rows or offsets are needed")
+        rows = columns
+    yt, ys = _codes(Yt, Ys, N, columns, N)
+    xt, xs = _codes(Xt, Xs, K, columns, K)
+    _check("sfl_quant_product_weights",
+           _lib.sfl_quant_product_weights(yt, ys, N, xt, xs, K, rows, columns, _buf(offsets, _I32, E + 1), E, dt,
+                                          _buf(dW, dt, E * N * K, K), _stream(stream)))
+
+
+def adamw_list(params, grads, m, v, *, halves=None, m_scales=None, v_scales=None, weight_decay=0.0):
+    """The list of tensors that sfl_adamw_step takes; it keeps them alive. Moments are fp32, or
+    float8_e4m3fn with uint8 scales of one for each 128 elements. weight_decay: one for all, or one
+    for each tensor; halves: bf16 copies, None for no copy (of all, or of single tensors)."""
+    n = len(params)
+    none = [None] * n
+    halves, m_scales, v_scales = halves or none, m_scales or none, v_scales or none
+    decay = [weight_decay] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
+    lists = (params, grads, m, v, halves, m_scales, v_scales, decay)
+    if any(len(x) != n for x in lists):
+        raise ValueError("the lists of sfl_adamw_step need one entry for each parameter")
+    a = (Adamw * n)()
+    for i, (p, g, mi, vi, half, ms, vs, wd) in enumerate(zip(*lists)):
+        e, pd, gd = p.numel(), dtype_code(p.dtype), dtype_code(g.dtype)
+        small = mi.dtype == torch.float8_e4m3fn
+        kind, blocks = (_F8, -(-e // 128)) if small else (_F32, 0)
+        if not small and (ms is not None or vs is not None):
+            raise ValueError("fp32 moments have no scales")
+        a[i] = Adamw(_buf(p, pd, e), _buf(g, gd, e), _buf(half, _BF16, e), _buf(mi, kind, e), _buf(vi, kind, e),
+                     _buf(ms, _U8, blocks), _buf(vs, _U8, blocks), e, wd, pd, gd,
+                     SFL_MOMENTS_8BIT if small else SFL_MOMENTS_F32)
+    a._keepalive = [tuple(x) for x in lists]  # the caller's lists may change
+    return a
+
+
+def sfl_adamw_step(tensors, step, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, sumsq=None, max_norm=0.0, norm=None,
+                   lr_scale=None, seed=0, stream=None):
+    cfg = AdamwCfg(lr, beta1, beta2, eps, max_norm, seed & 0xffffffff, 0, _buf(step, _I64, 1), _buf(lr_scale, _F32, 1),
+                   _buf(sumsq, _F64, 1), _buf(norm, _F32, 1))
+    _check("sfl_adamw_step", _lib.sfl_adamw_step(tensors, len(tensors), cfg, _stream(stream)))
 
 
 # ---- HIP events through the runtime library torch already loaded (for stage timing) ----

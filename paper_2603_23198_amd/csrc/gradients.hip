@@ -8,6 +8,7 @@
 // its end, where the first one stopped: the last 256 MiB that were read are still in the infinity
 // cache, and the scaled values are stored non-temporally beside them.
 #include "block.h"
+#include "clip.h"
 #include "rows.h"
 
 #include <algorithm>
@@ -139,17 +140,6 @@ __global__ __launch_bounds__(kSumThreads) void k_grad_sum(const double* __restri
   if (threadIdx.x == 0) *sumsq = s;
 }
 
-// A clipping coefficient, by 2^exp. exp is 0 where by alone is a normal fp32 number: a subnormal one has
-// fewer bits than the gradients (max_norm = 1e-3 of a norm of 3e38: 1e-4 off), and a smaller one is 0.
-struct Scale {
-  float by;
-  int exp;
-  __device__ __forceinline__ Scale(double c) : by((float)c), exp(0) {
-    if (c > 0 && c < 0x1p-126) by = (float)frexp(c, &exp);
-  }
-  __device__ __forceinline__ float operator()(float g) const { return ldexpf(g * by, exp); }
-};
-
 template <typename V> __device__ __forceinline__ void share_scale(const V* p, V* q, int n, const Scale& scale) {
   if (p == q && scale.by == 1.f && scale.exp == 0) return;
   using S = Step<V>;
@@ -170,9 +160,8 @@ template <int MAX>
 __global__ __launch_bounds__(kThreads) void k_grad_scale(GradList<MAX> l, const double* __restrict__ sumsq,
                                                          float max_norm, float* __restrict__ norm) {
   const double nrm = sqrt(*sumsq);
-  const float shown = (float)nrm;  // infinite where fp32 cannot hold it, and then nothing is scaled
-  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = shown;
-  const Scale by(nrm > (double)max_norm && shown < INFINITY ? (double)max_norm / nrm : 1.0);
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)nrm;
+  const Scale by(clip_coefficient(nrm, (double)max_norm));
   if (l.count == 0) return;
   const int b = gridDim.x - 1 - blockIdx.x, i = range_of(l, b);
   const int64_t at = (int64_t)(b - l.first[i]) * l.share;

@@ -7,7 +7,9 @@
 
 namespace {
 
-const char* const kNames[] = {"float32", "bfloat16", "int32", "float64"};  // SFL_F32, SFL_BF16, then by place
+// SFL_F32, SFL_BF16, then by place
+const char* const kNames[] = {"float32", "bfloat16", "int32", "float64", "float8_e4m3fn", "uint8", "int64"};
+constexpr long kKinds = sizeof(kNames) / sizeof(kNames[0]);
 
 bool is_kind(const at::Tensor& t, long kind) {
   switch (kind) {
@@ -15,6 +17,9 @@ bool is_kind(const at::Tensor& t, long kind) {
     case 1: return t.scalar_type() == at::kBFloat16;
     case 2: return t.scalar_type() == at::kInt;
     case 3: return t.scalar_type() == at::kDouble;
+    case 4: return t.scalar_type() == at::kFloat8_e4m3fn;
+    case 5: return t.scalar_type() == at::kByte;
+    case 6: return t.scalar_type() == at::kLong;
     default: return false;
   }
 }
@@ -72,7 +77,7 @@ PyObject* ptr(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     const long kind = PyLong_AsLong(a[1]);
     const long long n = PyLong_AsLongLong(a[2]), cols = nargs == 4 ? PyLong_AsLongLong(a[3]) : -1;
     if (PyErr_Occurred()) return nullptr;
-    if (kind < 0 || kind > 3) {
+    if (kind < 0 || kind >= kKinds) {
       PyErr_SetString(PyExc_ValueError, "unknown kind of tensor");
       return nullptr;
     }
