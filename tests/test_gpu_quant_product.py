@@ -1,0 +1,260 @@
+"""Products of 8-bit codes against float64 products of the numbers that the codes stand for."""
+import numpy as np
+import pytest
+import torch
+
+from block_util import DT, Out, U32, U_BF16, same_bits
+from oracle import routed as o
+from paper_2603_23198_amd import binding as b
+from routed_util import codes_on_gpu, run_offsets, up
+
+pytestmark = pytest.mark.gpu
+
+
+def operand(rng, rows, n, kind="normal"):
+    """Numbers [rows][n] with blocks of different magnitude."""
+    x = rng.normal(size=(rows, n))
+    if kind == "wide":  # within a block too
+        x = x * np.exp(rng.normal(size=(rows, n)) * 2)
+    return x * 2.0 ** rng.integers(-6, 7, size=(rows, 1))
+
+
+def assert_product(got, x, w, dt, name=""):
+    """got = x w^T. A sum of n exact products in fp32, in any order, is off by at most n 2^-23 of the
+    products' magnitudes (2^-23 a sum: it may be cut off rather than rounded). A bf16 result may come from
+    the 8-bit matrix instruction, which keeps 13 bits below the largest of eight neighbouring products:
+    of these eight each is off by at most 2^-13 of it."""
+    ref, size = x @ w.T, np.abs(x) @ np.abs(w).T
+    tol = x.shape[1] * 2 * U32 * size
+    if dt == "bf16":
+        n = up(x.shape[1], 8)
+        pad = ((0, 0), (0, n - x.shape[1]))
+        a, c = np.abs(np.pad(x, pad)).reshape(-1, n // 8, 8), np.abs(np.pad(w, pad)).reshape(-1, n // 8, 8)
+        largest = np.zeros_like(ref)
+        for g in range(n // 8):
+            largest += (a[:, None, g] * c[None, :, g]).max(2)
+        tol = tol + 8 * 2.0 ** -13 * largest
+        tol = tol + U_BF16 * (np.abs(ref) + tol)
+    err = np.abs(got - ref)
+    bad = ~(err <= tol + 1e-37)
+    assert not bad.any(), f"{name}: {bad.sum()} of {bad.size} out of bounds, worst {np.nanmax(err / (tol + 1e-37))}"
+
+
+def product(loads, K, N, dt, seed=0, first=0, rows=None, kind="normal", experts=None):
+    """Runs it; rows: room for more rows than the runs have."""
+    rng = np.random.default_rng(seed)
+    E, of = len(loads), run_offsets(loads, first)
+    T = of[0][-1] if rows is None else rows
+    Q, S, x = codes_on_gpu(*o.quant(operand(rng, max(T, 1), K, kind)[:T]))
+    W, Ws, w = [], [], []
+    for e in range(E):
+        q, ex = o.quant_square(operand(rng, N, K, kind))
+        q, s, v = codes_on_gpu(q, ex, 128)
+        W.append(q.view(torch.uint8))
+        Ws.append(s)
+        w.append(v)
+    W, Ws = torch.stack(W).view(Q.dtype), torch.stack(Ws)
+    Y = Out((T, N), DT[dt])
+    b.sfl_quant_product(Q, S, W, Ws, Y.t, offsets=of[1])
+    got = Y.values()
+    live = np.zeros(T, bool)
+    for e in range(E):
+        at = slice(of[0][e], of[0][e + 1])
+        live[at] = True
+        if loads[e]:
+            assert_product(got[at], x[at], w[e], dt, f"expert {e}")
+    assert (got[~live] == -77).all(), "rows of no expert"
+    return dict(Q=Q, S=S, W=W, Ws=Ws, Y=Y, offsets=of[1])
+
+
+SIZES = [(128, 1), (128, 16), (128, 130), (256, 64), (384, 100), (640, 257), (1024, 128), (2048, 40)]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("K,N", SIZES)
+@pytest.mark.parametrize("rows", [1, 2, 15, 17, 33, 64, 65, 128, 200, 300])
+def test_rows_of_one_expert(dt, K, N, rows):
+    product([rows], K, N, dt, seed=K + N + rows)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("loads", [[1, 1, 1, 1], [0, 3, 0, 16, 17], [64, 0, 65, 1], [130, 5, 0, 257, 31], [0, 0],
+                                   [1] * 70, [700, 2]])
+@pytest.mark.parametrize("K,N", [(128, 72), (384, 300)])
+def test_rows_of_several_experts(dt, loads, K, N):
+    product(loads, K, N, dt, seed=len(loads))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_rows_of_no_expert_are_left(dt):
+    product([20, 0, 33], 256, 96, dt, first=5, rows=100)
+    product([200, 0, 133], 256, 96, dt, first=5, rows=500)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [8, 400])
+def test_blocks_of_wide_range(dt, rows):
+    product([rows, rows // 2], 1280, 200, dt, kind="wide")
+
+
+@pytest.mark.parametrize("rows", [16, 300])
+def test_large_products(rows):
+    """Many tiles, long sums."""
+    product([rows, 3 * rows], 4096, 700, "f32", seed=3)
+    product([rows, 3 * rows], 4096, 700, "bf16", seed=3)
+
+
+def test_one_expert_without_offsets():
+    rng = np.random.default_rng(1)
+    Q, S, x = codes_on_gpu(*o.quant(operand(rng, 70, 256)))
+    W, Ws, w = codes_on_gpu(*o.quant_square(operand(rng, 90, 256)), 128)
+    Y = Out((70, 90), torch.float32)
+    b.sfl_quant_product(Q, S, W, Ws, Y.t)
+    assert_product(Y.values(), x, w, "f32")
+
+
+@pytest.mark.parametrize("rows", [5, 300])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_numbers_that_are_not_finite(dt, rows):
+    """A NaN code reaches its row of the result and no other."""
+    rng = np.random.default_rng(2)
+    xc, xe = o.quant(operand(rng, rows, 256))
+    wc, we = o.quant_square(operand(rng, 64, 256))
+    xc[rows // 2, 77] = 127
+    wc[9, 200] = 255
+    Q, S, x = codes_on_gpu(xc, xe)
+    W, Ws, w = codes_on_gpu(wc, we, 128)
+    Y = Out((rows, 64), DT[dt])
+    b.sfl_quant_product(Q, S, W, Ws, Y.t)
+    got = Y.values()
+    want = np.zeros((rows, 64), bool)
+    want[rows // 2], want[:, 9] = True, True
+    np.testing.assert_array_equal(np.isnan(got), want)
+    keep = np.arange(rows) != rows // 2
+    cols = np.arange(64) != 9
+    assert_product(got[keep][:, cols], x[keep], w[cols], dt)
+
+
+@pytest.mark.parametrize("rows", [5, 300])
+def test_scales_far_apart(rows):
+    """Scales up to 2^100 on one side and down to 2^-100 on the other."""
+    rng = np.random.default_rng(4)
+    xc, xe = o.quant(operand(rng, rows, 512))
+    wc, we = o.quant_square(operand(rng, 64, 512))
+    Q, S, x = codes_on_gpu(xc, xe + 95)
+    W, Ws, w = codes_on_gpu(wc, we - 95, 128)
+    for dt in ("bf16", "f32"):
+        Y = Out((rows, 64), DT[dt])
+        b.sfl_quant_product(Q, S, W, Ws, Y.t)
+        assert_product(Y.values(), x, w, dt)
+
+
+def test_offsets_without_meaning_stay_in_bounds():
+    rng = np.random.default_rng(5)
+    for T in (40, 400):
+        Q, S, _ = codes_on_gpu(*o.quant(operand(rng, T, 256)))
+        W, Ws, _ = codes_on_gpu(*o.quant_square(operand(rng, 3 * 128, 256)), 128)
+        W, Ws = W.view(torch.uint8).view(3, 128, 256).view(W.dtype), Ws.view(3, 1, 4)
+        Xt, Xs, _ = codes_on_gpu(*o.quant(operand(rng, 64, b.sfl_quant_columns(T, 3))))
+        for of in ([50, 20, 90, 10], [-5, 3000, 7, 1000], [0, T, 0, T], [1 << 30, -(1 << 30), 5, T]):
+            offsets = torch.tensor(of, dtype=torch.int32, device="cuda")
+            Y, dW = Out((T, 128), torch.bfloat16), Out((3, 64, 64), torch.float32)
+            b.sfl_quant_product(Q, S, W, Ws, Y.t, offsets=offsets)
+            b.sfl_quant_product_weights(Xt, Xs, Xt, Xs, dW.t, offsets=offsets)
+            Y.values(), dW.values()
+
+
+def weights(loads, N, K, dt, seed=0, first=0, kind="normal", T=None, wider=0):
+    rng = np.random.default_rng(seed)
+    of, offsets = run_offsets(loads, first)
+    T = T or max(of[-1], 1)
+    columns = b.sfl_quant_columns(T, len(loads)) + wider
+    sides = []
+    for n in (N, K):
+        c, e = o.quant_columns(operand(rng, T, n, kind), of)
+        # what lies behind the runs is NaN
+        codes, exps = np.full((n, columns), 127, np.uint8), np.full((n, columns // 128), 100)
+        codes[:, :c.shape[1]], exps[:, :e.shape[1]] = c, e
+        q, s, _ = codes_on_gpu(codes, exps)
+        sides.append((q, s, o.held(c, e)))
+    (Yt, Ys, y), (Xt, Xs, x) = sides
+    dW = Out((len(loads), N, K), DT[dt])
+    b.sfl_quant_product_weights(Yt, Ys, Xt, Xs, dW.t, offsets=offsets)
+    got, at = dW.values(), 0
+    for e, n in enumerate(loads):
+        if n == 0:
+            assert (got[e] == 0).all()
+            continue
+        assert_product(got[e], y[:, at:at + n], x[:, at:at + n], dt, f"expert {e}")
+        at += up(n)
+    return Yt, Ys, Xt, Xs, dW, offsets
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("loads", [[1], [128], [300, 0, 1], [0, 129, 0, 640], [0, 0], [90] * 9, [513, 127, 128, 1025]])
+@pytest.mark.parametrize("N,K", [(1, 1), (64, 64), (33, 200), (130, 257), (300, 128)])
+def test_gradients_of_weights(dt, loads, N, K):
+    weights(loads, N, K, dt, seed=N + K)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_gradients_of_weights_in_batches_of_fixed_room(dt):
+    weights([100, 31], 70, 90, dt, first=9, T=400, wider=512)
+    weights([300, 200, 500], 260, 520, dt, kind="wide")
+
+
+def test_one_run_of_columns_without_offsets():
+    rng = np.random.default_rng(1)
+    (Yt, Ys, y), (Xt, Xs, x) = (codes_on_gpu(*o.quant(operand(rng, n, 512))) for n in (40, 60))
+    dW = Out((1, 40, 60), torch.float32)
+    b.sfl_quant_product_weights(Yt, Ys, Xt, Xs, dW.t, rows=200)
+    assert_product(dW.values()[0], y[:, :256], x[:, :256], "f32")
+
+
+def test_repeats_graphs_and_streams():
+    """The same bits again, on another stream, and from captured calls whose offsets change."""
+    p = product([30, 3, 200], 384, 200, "bf16")
+    args = p["Q"], p["S"], p["W"], p["Ws"]
+    first = p["Y"].t.clone()
+    Yt, Ys, Xt, Xs, dW, offsets = weights([30, 3, 200], 100, 140, "f32")
+    dfirst = dW.t.clone()
+
+    def call():
+        b.sfl_quant_product(*args, p["Y"].t, offsets=p["offsets"])
+        b.sfl_quant_product_weights(Yt, Ys, Xt, Xs, dW.t, offsets=offsets)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        p["Y"].t.zero_()
+        dW.t.zero_()
+        call()
+    torch.cuda.synchronize()
+    assert same_bits(p["Y"].t, first) and same_bits(dW.t, dfirst)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for loads in ([30, 3, 200], [0, 33, 200], [100, 100, 33], [233, 0, 0]):
+        new = run_offsets(loads)[1]
+        p["offsets"].copy_(new)
+        offsets.copy_(new)
+        p["Y"].t.zero_()
+        dW.t.zero_()
+        call()
+        want = p["Y"].t.clone(), dW.t.clone()
+        p["Y"].t.zero_()
+        dW.t.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert same_bits(p["Y"].t, want[0]) and same_bits(dW.t, want[1])
+
+
+def test_a_row_does_not_depend_on_its_place():
+    """The same numbers as rows of one batch or of another of the same size: the same bits."""
+    rng = np.random.default_rng(7)
+    Q, S, _ = codes_on_gpu(*o.quant(operand(rng, 96, 640)))
+    W, Ws, _ = codes_on_gpu(*o.quant_square(operand(rng, 130, 640)), 128)
+    out = [torch.empty((96, 130), device="cuda") for _ in range(2)]
+    turn = torch.randperm(96, device="cuda")
+    b.sfl_quant_product(Q, S, W, Ws, out[0])
+    b.sfl_quant_product(Q.view(torch.uint8)[turn].view(Q.dtype), S[turn], W, Ws, out[1])
+    assert same_bits(out[0][turn], out[1])
