@@ -754,7 +754,8 @@ sfl_status_t sfl_quant_product(const uint8_t* Q, const uint8_t* S, int64_t rows,
  *           offsets
  *  dW       [E][N][K] dtype, overwritten; zeros for an expert without tokens
  *  rows     the tokens that the columns hold, or more (offsets are held to it), at most `columns`
- * N and K need not be multiples of anything. Errors as above (N, K <= 2^20). */
+ * N and K need not be multiples of anything. Errors as above; SFL_E_UNSUPPORTED for N or K > 2^20 or
+ * columns > 2^22. */
 sfl_status_t sfl_quant_product_weights(const uint8_t* Yt, const uint8_t* Ys, int64_t N, const uint8_t* Xt,
                                        const uint8_t* Xs, int64_t K, int64_t rows, int64_t columns,
                                        const int32_t* offsets, int32_t E, sfl_dtype_t dtype, void* dW,

@@ -104,8 +104,8 @@ sfl_status_t sfl_quant_product_weights(const uint8_t* Yt, const uint8_t* Ys, int
                                        sfl_stream_t stream) {
   sfl_status_t st = check_runs(rows, E);
   if (st == SFL_E_ARG || !dtype_ok(dtype) || K < 1 || N < 1 || (!offsets && E != 1)) return SFL_E_ARG;
-  if (st != SFL_OK || K > kMaxWidth8 || N > kMaxWidth8) return SFL_E_UNSUPPORTED;
-  if (columns % 512 || columns < rows || columns > INT32_MAX || !dW ||
+  if (st != SFL_OK || K > kMaxWidth8 || N > kMaxWidth8 || columns > kMaxColumns8) return SFL_E_UNSUPPORTED;
+  if (columns % 512 || columns < rows || !dW ||
       !aligned(dW, dtype == SFL_BF16 ? 2 : 4) || !aligned(Yt, 16) || !aligned(Xt, 16) || !aligned(Ys, 4) ||
       !aligned(Xs, 4) || (rows > 0 && (!Yt || !Ys || !Xt || !Xs)))
     return SFL_E_ARG;

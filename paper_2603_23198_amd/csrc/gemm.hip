@@ -21,6 +21,7 @@
 // active pre-activations straight from the accumulator registers (a ballot per register
 // and popcounts of its row group's bits, see twell_compact).
 #include "common.h"
+#include "direct.h"
 #include "internal.h"
 
 #include <algorithm>
@@ -70,7 +71,6 @@ __device__ __forceinline__ void zero_first(const GemmParams& p) {
 // All global reads go through raw buffer loads: an offset at or beyond the descriptor's
 // byte size reads as zero, so M/N/K tails and gathered rows need no branches. Offsets are
 // 32-bit, so every operand tensor must be smaller than 2 GiB (checked by the host).
-constexpr uint32_t kOOB = 0x80000000u;  // an offset that is always out of range
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, int64_t bytes) {
   const int32_t n = bytes > 0x7fffffff ? 0x7fffffff : (int32_t)bytes;
@@ -587,30 +587,6 @@ __host__ __device__ inline int splitk_count(int ksplit, int part_rows, int m_eff
   ks = min(ks, nk / 4);
   ks = min(ks, max(1, 512 / tiles));
   return max(ks, 1);
-}
-
-// The four descriptor words of a raw buffer resource, for inline assembly operands.
-__device__ __forceinline__ u32x4_t rsrc_words(const void* base, int64_t bytes) {
-  const uint64_t a = (uint64_t)(uintptr_t)base;
-  const uint32_t n = bytes > 0x7fffffff ? 0x7fffffffu : (uint32_t)bytes;
-  u32x4_t w;
-  w[0] = __builtin_amdgcn_readfirstlane((uint32_t)a);
-  w[1] = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32) & 0xffffu);  // stride 0
-  w[2] = n;
-  w[3] = 0x00020000u;
-  return w;
-}
-
-// 16 bytes per lane from a buffer straight into LDS at lds_off + 16 * lane. Written as
-// inline assembly: the compiler does not count these loads and so does not make every
-// later LDS read wait for all of them; the K loop waits for them itself (s_waitcnt vmcnt)
-// and orders them with barriers. Counting stays safe for the compiler's own loads: loads
-// complete in order, so extra loads in flight only make its waits stricter.
-__device__ __forceinline__ void load_lds16(u32x4_t rsrc, uint32_t lds_off, uint32_t voff, uint32_t soff) {
-  asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds"
-               :
-               : "v"(voff), "s"(rsrc), "s"(soff), "{m0}"(lds_off)
-               : "memory");
 }
 
 // One output tile (tm, tn) over K steps [kt0, kt1); SPLIT with ks > 1 stores the fp32
@@ -1273,20 +1249,6 @@ __global__ __launch_bounds__(NTHR) void k_gemm_few_rows(GemmParams p) {
     }
   }
   if (threadIdx.x == 0) p.tile_sem[n0 / TN] = 0;
-}
-
-// Compute units of the current device (cached per device; threads that race on the first
-// query store the same value).
-int device_cus() {
-  static std::atomic<int> cus[64];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
-  int n = cus[dev].load(std::memory_order_relaxed);
-  if (n <= 0) {
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
-    cus[dev].store(n, std::memory_order_relaxed);
-  }
-  return n;
 }
 
 // Rows per output tile of the TwELL GEMM: the height whose rounds of one tile per CU cost

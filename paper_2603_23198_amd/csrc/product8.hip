@@ -6,6 +6,7 @@
 // instructions are not: they add the products of eight neighbouring k with 13 bits below the largest of
 // them, 1.6e-5 of the result's magnitude for normal operands, by measurement.)
 #include "blocks8.h"
+#include "direct.h"
 #include "rows.h"
 
 #include <algorithm>
@@ -23,120 +24,485 @@ __device__ __forceinline__ bf16x8_t decode8(uint32_t lo, uint32_t hi, float by) 
   return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// One tile of a result: pointers to its first row and column.
-struct Tile {
-  const uint8_t* A;
-  const uint8_t* As;
-  const uint8_t* B;
-  const uint8_t* Bs;
-  int64_t lda, ldb, lsa, lsb;  // bytes between rows of codes and of scales
-  int m, n;                    // rows and columns that are there
-  int blocks;
-  int bshift;                  // 7: rows of B share scales by 128
-  int b0;                      // row of B, for them
+// A buffer of so many bytes, of values that are the same in every lane.
+__device__ __forceinline__ u32x4_t buffer_of(const void* base, int64_t bytes) {
+  u32x4_t w = rsrc_words(base, bytes);
+  w[2] = __builtin_amdgcn_readfirstlane(w[2]);
+  return w;
+}
+
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+
+// ---- tiles of 256 or 128 rows by 256 columns ---------------------------------------------
+// Eight waves, 2 along the rows x 4 along the columns, 128 (64) x 64 results each. A step is one block of
+// 128 k: both operands come straight from memory into LDS (one 128-byte line a row), into a ring of two
+// stages (three where tiles are 128 rows high), the next ones in flight while one feeds the matrix cores.
+// Chunk c (16 k) of row r lies at position c ^ swizzle(r), so that the 8 lanes of a fragment read's phase
+// meet 8 different positions. Scales travel the same way, a word of four blocks per row.
+// A workgroup stays on its CU and takes tile after tile; the next tile's first stage is on its way while
+// the results of one are stored.
+constexpr int kTileN = 256, kTileThreads = 512, kTileWaves = 8, kStep = 128;
+constexpr int kWordRing = 4;  // scale words: the one in use, and up to two ahead of it
+
+template <int BMT> struct Geo {
+  static constexpr int LA = BMT * kStep / 1024 / kTileWaves, LB = kTileN * kStep / 1024 / kTileWaves;
+  static constexpr int A = BMT * kStep, STAGE = (BMT + kTileN) * kStep, NS = BMT == 256 ? 2 : 3;
+  static constexpr int WORDS = (BMT + kTileN) * 4;           // bytes of a scale word of all rows
+  static constexpr int TM = BMT / 2 / 16, TN = 4;            // 16 x 16 results of a wave
+  static constexpr int SMEM = NS * STAGE + kWordRing * WORDS;
 };
 
-constexpr int kThreads = 256, kM = 64, kN = 64;
+// Of the columns' rows (B) two neighbouring fragments hold eight neighbouring columns per lane in a bf16
+// result (see column_of): their rows 0 .. 3 and 8 .. 11 are read together.
+template <bool PAIRED> __device__ __forceinline__ int swizzle_b(int row) {
+  return PAIRED ? (row & 3) | (row >> 1 & 4) : row & 7;
+}
+// Column, of a wave's 64, of row r of fragment j. The result has columns r = 4 g .. 4 g + 3 of a row in one
+// lane, and stores 16 bytes: 4 fp32 or, of two fragments, 8 bf16, 64 bytes of a row by four lanes.
+template <bool PAIRED> __device__ __forceinline__ int column_of(int j, int r) {
+  return PAIRED ? (j >> 1) * 32 + (r >> 2) * 8 + (j & 1) * 4 + (r & 3) : j * 16 + r;
+}
 
-// 64 x 64 by four waves of 16 rows; operands straight from memory.
-template <typename V>
-__device__ __forceinline__ void simple_tile(const Tile& t, V* C, int64_t ldc) {
+// What a workgroup needs of one tile.
+struct Where {
+  u32x4_t ra, rb, rs;          // buffers of the operands, and of this wave's scales
+  uint32_t offs;               // of this lane's scale row
+  int blocks, b0;              // steps, and the first block's place in its scale word
+  int m, n;                    // rows and columns that are there
+  char* C;
+  int64_t ldc;
+};
+
+template <int BMT, bool PAIRED> struct Loader {
+  typedef Geo<BMT> G;
+  int lane, wave;
+  uint32_t lds;
+  uint32_t offa[G::LA], offb[G::LB];
+  int stage_in = 0, word_in = 0;  // where the next stage and the next scale word go
+
+  __device__ __forceinline__ explicit Loader(const uint8_t* smem) {
+    lane = lane_id();
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    lds = __builtin_amdgcn_readfirstlane(
+        (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)smem);
+  }
+  // Load q of this wave fills rows (wave L + q) 8 .. + 7 of an operand's tile, a line of 128 bytes each.
+  __device__ __forceinline__ void setup(const Where& w, uint32_t lda, uint32_t ldb) {
+#pragma unroll
+    for (int q = 0; q < G::LA; ++q) {
+      const int row = (wave * G::LA + q) * 8 + (lane >> 3);
+      offa[q] = row < w.m ? (uint32_t)row * lda + ((lane & 7) ^ (row & 7)) * 16 : kOOB;
+    }
+#pragma unroll
+    for (int q = 0; q < G::LB; ++q) {
+      const int row = (wave * G::LB + q) * 8 + (lane >> 3);
+      offb[q] = row < w.n ? (uint32_t)row * ldb + ((lane & 7) ^ swizzle_b<PAIRED>(row)) * 16 : kOOB;
+    }
+  }
+  __device__ __forceinline__ void issue(const Where& w, int kt) {
+    const uint32_t at = lds + stage_in * G::STAGE, k = (uint32_t)kt * kStep;
+#pragma unroll
+    for (int q = 0; q < G::LA; ++q) load_lds16(w.ra, at + (wave * G::LA + q) * 1024, offa[q], k);
+#pragma unroll
+    for (int q = 0; q < G::LB; ++q) load_lds16(w.rb, at + G::A + (wave * G::LB + q) * 1024, offb[q], k);
+    stage_in = stage_in == G::NS - 1 ? 0 : stage_in + 1;
+    if (kt == 0 || ((w.b0 + kt) & 3) == 0) {
+      // waves 0 .. BMT / 64 - 1 bring the rows' scales, waves 4 .. 7 the columns'
+      const int first = wave < 4 ? wave * 64 : BMT + (wave - 4) * 64;
+      if (wave >= 4 || wave * 64 < BMT)
+        load_lds4(w.rs, lds + G::NS * G::STAGE + word_in * G::WORDS + first * 4, w.offs, (uint32_t)((w.b0 + kt) >> 2) * 4);
+      word_in = (word_in + 1) & (kWordRing - 1);
+    }
+  }
+  __device__ __forceinline__ void prologue(const Where& w) {
+#pragma unroll
+    for (int i = 0; i < G::NS - 1; ++i)
+      if (i < w.blocks) issue(w, i);
+  }
+};
+
+// The tile's sums. EXACT: in bf16, with exact products; else on the 8-bit instruction.
+template <int BMT, bool PAIRED, bool EXACT> struct Worker {
+  typedef Geo<BMT> G;
+  f32x4_t acc[G::TM][G::TN];
+  int stage = 0, word = 0;
+  uint32_t sa[G::TM], sb[G::TN];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < G::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < G::TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  static __device__ __forceinline__ i32x8_t fragment(const uint8_t* rows, int row, int swizzle, int g) {
+    const u32x4_t lo = *(const u32x4_t*)(rows + row * kStep + (g ^ swizzle) * 16);
+    const u32x4_t hi = *(const u32x4_t*)(rows + row * kStep + ((g + 4) ^ swizzle) * 16);
+    return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  }
+  __device__ __forceinline__ void step(const uint8_t* smem, int wm, int wn, int lane, int b, bool first) {
+    const int x = lane & 15, g = lane >> 4;
+    const uint8_t *As = smem + stage * G::STAGE, *Bs = As + G::A;
+    if (first || (b & 3) == 0) {
+      const uint32_t* w = (const uint32_t*)(smem + G::NS * G::STAGE + word * G::WORDS);
+#pragma unroll
+      for (int i = 0; i < G::TM; ++i) sa[i] = w[wm * (BMT / 2) + i * 16 + x] >> (b & 3) * 8;
+#pragma unroll
+      for (int j = 0; j < G::TN; ++j) sb[j] = w[BMT + wn * 64 + column_of<PAIRED>(j, x)] >> (b & 3) * 8;
+      word = (word + 1) & (kWordRing - 1);
+    } else {
+#pragma unroll
+      for (int i = 0; i < G::TM; ++i) sa[i] >>= 8;
+#pragma unroll
+      for (int j = 0; j < G::TN; ++j) sb[j] >>= 8;
+    }
+    if constexpr (EXACT) {
+      bf16x8_t bw[G::TN][4];
+#pragma unroll
+      for (int j = 0; j < G::TN; ++j) {
+        const int row = wn * 64 + column_of<PAIRED>(j, x);
+        const i32x8_t w = fragment(Bs, row, swizzle_b<PAIRED>(row), g);
+        const float by = scale8(sb[j] & 0xff);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) bw[j][q] = decode8(w[2 * q], w[2 * q + 1], by);
+      }
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int i = 0; i < G::TM; ++i) {
+        const int row = wm * (BMT / 2) + i * 16 + x;
+        const i32x8_t a = fragment(As, row, row & 7, g);
+        const float by = scale8(sa[i] & 0xff);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const bf16x8_t aw = decode8(a[2 * q], a[2 * q + 1], by);
+#pragma unroll
+          for (int j = 0; j < G::TN; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[j][q], aw, acc[i][j], 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_s_setprio(0);
+    } else {
+      i32x8_t bw[G::TN];
+#pragma unroll
+      for (int j = 0; j < G::TN; ++j) {
+        const int row = wn * 64 + column_of<PAIRED>(j, x);
+        bw[j] = fragment(Bs, row, swizzle_b<PAIRED>(row), g);
+      }
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int i = 0; i < G::TM; ++i) {
+        const int row = wm * (BMT / 2) + i * 16 + x;
+        const i32x8_t a = fragment(As, row, row & 7, g);
+#pragma unroll
+        for (int j = 0; j < G::TN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bw[j], a, acc[i][j], 0, 0, 0, (int)sb[j], 0,
+                                                                       (int)sa[i]);
+      }
+      __builtin_amdgcn_s_setprio(0);
+    }
+    stage = stage == G::NS - 1 ? 0 : stage + 1;
+  }
+  template <typename V> __device__ __forceinline__ void store(const Where& w, int wm, int wn, int lane) const {
+    constexpr int each = 16 / sizeof(V);
+    const int x = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < G::TM; ++i) {
+      const int m = wm * (BMT / 2) + i * 16 + x;
+      if (m >= w.m) continue;
+      V* row = (V*)w.C + m * w.ldc;
+#pragma unroll
+      for (int j = 0; j < G::TN; j += PAIRED ? 2 : 1) {
+        const int n = wn * 64 + column_of<PAIRED>(j, 4 * g);
+        u32x4_t out;
+        if constexpr (PAIRED) {
+          const f32x4_t &a = acc[i][j], &c = acc[i][j + 1];
+          out = u32x4_t{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(c[0], c[1]), pack_bf16(c[2], c[3])};
+        } else {
+          __builtin_memcpy(&out, &acc[i][j], 16);
+        }
+        if (n + each <= w.n) {
+          store16(row + n, out);
+        } else {
+          V v[each];
+          __builtin_memcpy(v, &out, 16);
+#pragma unroll
+          for (int e = 0; e < each; ++e)
+            if (n + e < w.n) row[n + e] = v[e];
+        }
+      }
+    }
+  }
+};
+
+// before[e]: units of `size` rows in the runs before run e, up to before[E]; by the first wave.
+__device__ __forceinline__ void count_units(const int32_t* __restrict__ offsets, int E, int rows, int size, int* before) {
+  if (threadIdx.x >= kWave) return;
+  const int lane = lane_id(), per = (E + kWave - 1) / kWave, e0 = min(lane * per, E), e1 = min(e0 + per, E);
+  int n = 0;
+  for (int e = e0; e < e1; ++e) {
+    const int len = offsets ? max(offset8(offsets, e + 1, rows) - offset8(offsets, e, rows), 0) : rows;
+    before[e] = n;
+    n += (len + size - 1) / size;
+  }
+  const int incl = wave_incl_scan(n);
+  for (int e = e0; e < e1; ++e) before[e] += incl - n;
+  if (lane == kWave - 1) before[E] = incl;
+}
+
+// Tile `id` of tiles_m x tiles_n: neighbouring workgroups are on different XCDs, so each XCD (id % 8) gets a
+// run of tiles, walked in groups of 8 rows of tiles so that its L2 serves them. false: no such tile.
+__device__ __forceinline__ bool tile_at(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
+  const uint32_t total = tiles_m * tiles_n, run = (total + 7) / 8, at = id / 8, v = id % 8 * run + at;
+  if (at >= run || v >= total) return false;
+  const uint32_t first = v / (8 * tiles_n) * 8, high = min(tiles_m - first, 8u), in = v - first * tiles_n;
+  tn = in / high;
+  tm = first + in - tn * high;
+  return true;
+}
+
+// WEIGHTS: results are the weights' gradients of expert after expert; else the rows of run after run.
+template <int BMT, bool EXACT, bool WEIGHTS, typename V>
+__global__ __launch_bounds__(kTileThreads) void k_product8_tiles(Product8 p) {
+  constexpr bool PAIRED = sizeof(V) == 2;
+  typedef Geo<BMT> G;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[G::SMEM];
+  __shared__ int before[kMaxExperts8 + 1];
+  const int rows = (int)p.rows;
+  count_units(p.offsets, p.E, rows, WEIGHTS ? kBlock8 : BMT, before);
+  __syncthreads();
+  const uint32_t tiles_n = (uint32_t)cdiv(WEIGHTS ? p.K : p.N, kTileN), each = (uint32_t)cdiv(p.N, BMT);
+  const uint32_t tiles_m = __builtin_amdgcn_readfirstlane(WEIGHTS ? p.E * each : (uint32_t)before[p.E]);
+  const uint32_t limit = (tiles_m * tiles_n + 7) / 8 * 8;
+  const int64_t ld = WEIGHTS ? p.columns : p.K, ls = WEIGHTS ? p.columns / kBlock8 : scale_row8(p.K);
+  Loader<BMT, PAIRED> load(smem);
+  const int lane = load.lane, wave = load.wave, wm = wave & 1, wn = wave >> 1;
+
+  auto find = [&](uint32_t id, Where& w) {  // the tile at id or later of this workgroup's
+    uint32_t tm, tn;
+    for (; id < limit; id += gridDim.x)
+      if (tile_at(id, tiles_m, tiles_n, tm, tn)) break;
+    if (id >= limit) return id;
+    const uint8_t *A, *As, *B, *Bs;
+    int bshift = 0;
+    if constexpr (WEIGHTS) {
+      const uint32_t e = tm / each;
+      const int64_t m0 = (int64_t)(tm - e * each) * BMT, n0 = (int64_t)tn * kTileN;
+      const int b = before[e];
+      w.m = (int)min((int64_t)BMT, p.N - m0);
+      w.n = (int)min((int64_t)kTileN, p.K - n0);
+      w.blocks = max(min(before[e + 1] - b, (int)ls - b), 0);
+      w.b0 = b & 3;
+      A = p.A + m0 * ld + (int64_t)b * kBlock8;
+      B = p.B + n0 * ld + (int64_t)b * kBlock8;
+      As = p.As + m0 * ls + (b - w.b0);
+      Bs = p.Bs + n0 * ls + (b - w.b0);
+      w.C = (char*)p.C + ((e * p.N + m0) * p.K + n0) * (int64_t)sizeof(V);
+      w.ldc = p.K;
+    } else {
+      int lo = 0, hi = p.E - 1;  // the last run with before[e] <= tm; it has units
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (before[mid] <= (int)tm)
+          lo = mid;
+        else
+          hi = mid - 1;
+      }
+      const int e = __builtin_amdgcn_readfirstlane(lo);
+      const int run = p.offsets ? offset8(p.offsets, e, rows) : 0, end = p.offsets ? offset8(p.offsets, e + 1, rows) : rows;
+      const int64_t m0 = run + (int64_t)((int)tm - before[e]) * BMT, n0 = (int64_t)tn * kTileN;
+      w.m = (int)min((int64_t)BMT, end - m0);
+      w.n = (int)min((int64_t)kTileN, p.N - n0);
+      w.blocks = (int)(p.K / kBlock8);
+      w.b0 = 0;
+      A = p.A + m0 * ld;
+      As = p.As + m0 * ls;
+      B = p.B + (e * p.N + n0) * ld;
+      Bs = p.Bs + (e * blocks8(p.N) + n0 / kBlock8) * ls;
+      bshift = 7;
+      w.C = (char*)p.C + (m0 * p.N + n0) * (int64_t)sizeof(V);
+      w.ldc = p.N;
+    }
+    w.m = __builtin_amdgcn_readfirstlane(w.m);
+    w.n = __builtin_amdgcn_readfirstlane(w.n);
+    w.blocks = __builtin_amdgcn_readfirstlane(w.blocks);
+    w.b0 = __builtin_amdgcn_readfirstlane(w.b0);
+    w.ra = buffer_of(A, w.m * ld);
+    w.rb = buffer_of(B, w.n * ld);
+    const int row = (wave & 3) * 64 + lane;
+    w.rs = wave < 4 ? buffer_of(As, w.m * ls) : buffer_of(Bs, (((w.n - 1) >> bshift) + 1) * ls);
+    w.offs = row < (wave < 4 ? w.m : w.n) ? (uint32_t)(wave < 4 ? row : row >> bshift) * (uint32_t)ls : kOOB;
+    return id;
+  };
+
+  Where w;
+  uint32_t id = find(blockIdx.x, w);
+  if (id >= limit) return;
+  Worker<BMT, PAIRED, EXACT> work;
+  load.setup(w, (uint32_t)ld, (uint32_t)ld);
+  load.prologue(w);
+  for (;;) {
+    work.clear();
+    for (int kt = 0; kt < w.blocks; ++kt) {
+      // this stage has landed (of three, the next may still be on its way) and this wave's reads of the
+      // last one are done; after the barrier that holds for all waves, and its place may be filled again
+      static_assert(G::LA + G::LB < 16, "the wait's low bits");
+      if (G::NS == 3 && kt + 1 < w.blocks)
+        __builtin_amdgcn_s_waitcnt(0x0070 | (G::LA + G::LB));
+      else
+        __builtin_amdgcn_s_waitcnt(0x0070);
+      __syncthreads();
+      if (kt + G::NS - 1 < w.blocks) load.issue(w, kt + G::NS - 1);
+      work.step(smem, wm, wn, lane, w.b0 + kt, kt == 0);
+    }
+    Where next;
+    const uint32_t id2 = find(id + gridDim.x, next);
+    if (id2 < limit) {
+      load.setup(next, (uint32_t)ld, (uint32_t)ld);
+      load.prologue(next);
+    }
+    work.template store<V>(w, wm, wn, lane);
+    if (id2 >= limit) break;
+    w = next;
+    id = id2;
+  }
+}
+
+// ---- few rows of an expert: its weights pass by once ---------------------------------------
+// A wave has 16 columns and up to 16 MT rows, its operands come from memory into registers: bound by the
+// weights' bytes, so the products are the exact ones in bf16. The KS waves that share columns have a part
+// of the blocks each and add their sums over LDS, in order; so few columns still fill the chip.
+constexpr int kStreamThreads = 512, kStreamWaves = kStreamThreads / kWave;
+
+template <int MT, int KS, typename V>
+__global__ __launch_bounds__(kStreamThreads) void k_product8_stream(Product8 p, int64_t units) {
+  constexpr int STRIPS = kStreamWaves / KS, UNROLL = MT == 1 ? 4 : 2;
+  __shared__ f32x4_t part[KS > 1 ? kStreamWaves : 1][MT][kWave];
   const int lane = lane_id(), wave = threadIdx.x / kWave, x = lane & 15, g = lane >> 4;
-  const int m = min(wave * 16 + x, t.m - 1);
-  f32x4_t acc[4] = {};
-  for (int b = 0; b < t.blocks; ++b) {
-    uint32_t a[8], w[8];
-    __builtin_memcpy(a, t.A + m * t.lda + b * 128 + g * 32, 32);
-    const float sa = scale8(t.As[m * t.lsa + b]);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int n = min(j * 16 + x, t.n - 1);
-      __builtin_memcpy(w, t.B + n * t.ldb + b * 128 + g * 32, 32);
-      const float sb = scale8(t.Bs[(int64_t)((t.b0 + n) >> t.bshift) * t.lsb + b]);
-#pragma unroll
-      for (int q = 0; q < 4; ++q)  // lane: row x of A, columns 4 g .. 4 g + 3
-        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(w[2 * q], w[2 * q + 1], sb),
-                                                         decode8(a[2 * q], a[2 * q + 1], sa), acc[j], 0, 0, 0);
-    }
-  }
-  if (wave * 16 + x >= t.m) return;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int n = j * 16 + g * 4 + i;
-      if (n < t.n) VT<V>::store(C, m * ldc + n, acc[j][i]);
-    }
-}
-
-template <typename V> __global__ __launch_bounds__(kThreads) void k_product8(Product8 p, int64_t mtiles) {
-  const int64_t ntiles = cdiv(p.N, kN), total = mtiles * ntiles, sk = scale_row8(p.K);
+  const int ks = wave % KS, strip = wave / KS, rows = (int)p.rows;
+  const int64_t strips = cdiv(p.N, 16 * STRIPS), total = units * strips, sk = scale_row8(p.K);
+  const int blocks = (int)(p.K / kBlock8), k0 = (int)((int64_t)blocks * ks / KS), k1 = (int)((int64_t)blocks * (ks + 1) / KS);
   for (int64_t id = blockIdx.x; id < total; id += gridDim.x) {
-    const int64_t mt = id / ntiles;
-    const int nt = (int)(id - mt * ntiles);
-    const Unit u = unit_of(p.offsets, p.E, (int)p.rows, kM, (int)mt);
+    const int64_t unit = id / strips, n0 = ((id - unit * strips) * STRIPS + strip) * 16;
+    const Unit u = unit_of(p.offsets, p.E, rows, 16 * MT, (int)unit);
     if (u.expert < 0) return;
-    Tile t;
-    t.A = p.A + u.first * p.K;
-    t.As = p.As + u.first * sk;
-    t.B = p.B + ((int64_t)u.expert * p.N + nt * kN) * p.K;
-    t.Bs = p.Bs + u.expert * blocks8(p.N) * sk;
-    t.lda = t.ldb = p.K;
-    t.lsa = t.lsb = sk;
-    t.m = u.count;
-    t.n = (int)min((int64_t)kN, p.N - (int64_t)nt * kN);
-    t.blocks = (int)(p.K / kBlock8);
-    t.bshift = 7;
-    t.b0 = nt * kN;
-    simple_tile(t, (V*)p.C + u.first * p.N + nt * kN, p.N);
-  }
-}
-
-template <typename V> __global__ __launch_bounds__(kThreads) void k_product8_weights(Product8 p) {
-  const int64_t mtiles = cdiv(p.N, kM), ntiles = cdiv(p.K, kN), total = p.E * mtiles * ntiles, ss = p.columns / kBlock8;
-  for (int64_t id = blockIdx.x; id < total; id += gridDim.x) {
-    const int e = (int)(id / (mtiles * ntiles));
-    const int64_t rest = id - e * mtiles * ntiles, mt = rest / ntiles, nt = rest - mt * ntiles;
-    const Run r = run_of(p.offsets, (int)p.rows, kBlock8, e);
-    Tile t;
-    t.A = p.A + mt * kM * p.columns + (int64_t)r.before * kBlock8;
-    t.As = p.As + mt * kM * ss + r.before;
-    t.B = p.B + nt * kN * p.columns + (int64_t)r.before * kBlock8;
-    t.Bs = p.Bs + nt * kN * ss + r.before;
-    t.lda = t.ldb = p.columns;
-    t.lsa = t.lsb = ss;
-    t.m = (int)min((int64_t)kM, p.N - mt * kM);
-    t.n = (int)min((int64_t)kN, p.K - nt * kN);
-    t.blocks = (int)min(blocks8(r.count), max(ss - r.before, (int64_t)0));
-    t.bshift = 0;
-    t.b0 = 0;
-    simple_tile(t, (V*)p.C + ((int64_t)e * p.N + mt * kM) * p.K + nt * kN, p.K);
+    const int64_t n = min(n0 + x, p.N - 1);
+    const uint8_t* B = p.B + (u.expert * p.N + n) * p.K + g * 16;
+    const uint8_t* Bs = p.Bs + (u.expert * blocks8(p.N) + n / kBlock8) * sk;
+    const uint8_t *A[MT], *As[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int64_t m = u.first + min(i * 16 + x, u.count - 1);
+      A[i] = p.A + m * p.K + g * 16;
+      As[i] = p.As + m * sk;
+    }
+    f32x4_t acc[MT] = {};
+    for (int b0 = k0; b0 < k1; b0 += UNROLL) {
+      u32x4_t w[UNROLL][2], a[UNROLL][MT][2];
+      int sb[UNROLL], sa[UNROLL][MT];
+#pragma unroll
+      for (int q = 0; q < UNROLL; ++q) {
+        const int b = min(b0 + q, k1 - 1);
+        w[q][0] = *(const u32x4_t*)(B + (int64_t)b * kBlock8);
+        w[q][1] = *(const u32x4_t*)(B + (int64_t)b * kBlock8 + 64);
+        sb[q] = Bs[b];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+          if (i * 16 < u.count) {
+            a[q][i][0] = *(const u32x4_t*)(A[i] + (int64_t)b * kBlock8);
+            a[q][i][1] = *(const u32x4_t*)(A[i] + (int64_t)b * kBlock8 + 64);
+            sa[q][i] = As[i][b];
+          }
+      }
+#pragma unroll
+      for (int q = 0; q < UNROLL; ++q) {
+        if (b0 + q >= k1) break;
+        bf16x8_t bw[4];
+        const float by = scale8(sb[q]);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) bw[h] = decode8(w[q][h / 2][h % 2 * 2], w[q][h / 2][h % 2 * 2 + 1], by);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+          if (i * 16 < u.count) {
+            const float bya = scale8(sa[q][i]);
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+              acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  bw[h], decode8(a[q][i][h / 2][h % 2 * 2], a[q][i][h / 2][h % 2 * 2 + 1], bya), acc[i], 0, 0, 0);
+          }
+      }
+    }
+    if (KS > 1) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) part[wave][i][lane] = acc[i];
+      __syncthreads();
+      if (ks == 0)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+          for (int q = 1; q < KS; ++q) acc[i] += part[wave + q][i][lane];
+      __syncthreads();
+    }
+    if (ks == 0)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int m = i * 16 + x;
+        if (m >= u.count) continue;
+        V* row = (V*)p.C + (u.first + m) * p.N;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (n0 + 4 * g + e < p.N) VT<V>::store(row, n0 + 4 * g + e, acc[i][e]);
+      }
   }
 }
 
 dim3 grid_of(int64_t tiles, int threads) { return dim3((unsigned)std::min<int64_t>(tiles, max_blocks(threads))); }
 
-}  // namespace
-
-hipError_t launch_product8(const Product8& p, int bf16, hipStream_t s) {
-  // every run ends in a tile that may not be full
-  const int64_t mtiles = p.offsets ? std::min(p.rows, p.rows / kM + p.E) : cdiv(p.rows, kM);
-  const dim3 grid = grid_of(mtiles * cdiv(p.N, kN), kThreads);
-  if (mtiles == 0) return hipSuccess;
-  if (bf16)
-    hipLaunchKernelGGL(k_product8<bf16_t>, grid, dim3(kThreads), 0, s, p, mtiles);
-  else
-    hipLaunchKernelGGL(k_product8<float>, grid, dim3(kThreads), 0, s, p, mtiles);
+template <int BMT, bool EXACT, bool WEIGHTS, typename V> hipError_t tiles(const Product8& p, int64_t count, hipStream_t s) {
+  if (count > INT32_MAX - 8) return hipErrorInvalidValue;  // of 2^15 results or more each: beyond any memory
+  const unsigned grid = (unsigned)std::min<int64_t>(up(count, 8), up(device_cus(), 8));
+  hipLaunchKernelGGL((k_product8_tiles<BMT, EXACT, WEIGHTS, V>), dim3(grid), dim3(kTileThreads), 0, s, p);
   return hipGetLastError();
 }
 
-hipError_t launch_product8_weights(const Product8& p, int bf16, hipStream_t s) {
-  const dim3 grid = grid_of(p.E * cdiv(p.N, kM) * cdiv(p.K, kN), kThreads);
+template <int MT, int KS> hipError_t stream(const Product8& p, int bf16, int64_t units, hipStream_t s) {
+  const dim3 grid = grid_of(units * cdiv(p.N, 16 * (kStreamWaves / KS)), kStreamThreads);
   if (bf16)
-    hipLaunchKernelGGL(k_product8_weights<bf16_t>, grid, dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((k_product8_stream<MT, KS, bf16_t>), grid, dim3(kStreamThreads), 0, s, p, units);
   else
-    hipLaunchKernelGGL(k_product8_weights<float>, grid, dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((k_product8_stream<MT, KS, float>), grid, dim3(kStreamThreads), 0, s, p, units);
   return hipGetLastError();
+}
+
+// Units that any runs of `rows` rows in all take: every run ends in one that may not be full.
+int64_t most_units(const Product8& p, int64_t size) {
+  return p.offsets ? std::min(p.rows, p.rows / size + p.E) : cdiv(p.rows, size);
+}
+
+}  // namespace
+
+hipError_t launch_product8(const Product8& p, int bf16, hipStream_t s) {
+  const int64_t live = std::min<int64_t>(p.E, p.rows);
+  if (p.rows <= 64 * live) {
+    const int64_t waves = live * cdiv(p.N, 16), want = (int64_t)device_cus() * 8;
+    const int ks = waves * 8 <= want ? 8 : waves * 4 <= want ? 4 : waves * 2 <= want ? 2 : 1;
+    if (p.rows <= 16) {
+      const int64_t units = most_units(p, 16);
+      return ks == 8 ? stream<1, 8>(p, bf16, units, s) : ks == 4 ? stream<1, 4>(p, bf16, units, s)
+           : ks == 2 ? stream<1, 2>(p, bf16, units, s) : stream<1, 1>(p, bf16, units, s);
+    }
+    const int64_t units = most_units(p, 64);
+    return ks == 8 ? stream<4, 8>(p, bf16, units, s) : ks == 4 ? stream<4, 4>(p, bf16, units, s)
+         : ks == 2 ? stream<4, 2>(p, bf16, units, s) : stream<4, 1>(p, bf16, units, s);
+  }
+  const bool high = p.rows / p.E >= 512;
+  const int64_t count = most_units(p, high ? 256 : 128) * cdiv(p.N, kTileN);
+  if (bf16) return high ? tiles<256, false, false, bf16_t>(p, count, s) : tiles<128, false, false, bf16_t>(p, count, s);
+  return high ? tiles<256, true, false, float>(p, count, s) : tiles<128, true, false, float>(p, count, s);
+}
+
+hipError_t launch_product8_weights(const Product8& p, int bf16, hipStream_t s) {
+  const int64_t high = p.E * cdiv(p.N, 256) * cdiv(p.K, kTileN), low = p.E * cdiv(p.N, 128) * cdiv(p.K, kTileN);
+  if (high >= device_cus())
+    return bf16 ? tiles<256, false, true, bf16_t>(p, high, s) : tiles<256, true, true, float>(p, high, s);
+  return bf16 ? tiles<128, false, true, bf16_t>(p, low, s) : tiles<128, true, true, float>(p, low, s);
 }
 
 }  // namespace sfl

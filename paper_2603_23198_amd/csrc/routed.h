@@ -18,6 +18,7 @@ hipError_t launch_route_groups_bwd(const sfl_route_groups_bwd_args_t& a, hipStre
 constexpr int kBlock8 = 128;           // elements that share a scale
 constexpr int kMaxExperts8 = 1024;
 constexpr int64_t kMaxWidth8 = 1 << 20;
+constexpr int64_t kMaxColumns8 = 1 << 22;  // of a product: 256 rows of them lie within 32-bit offsets
 
 constexpr int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 constexpr int64_t blocks8(int64_t n) { return (n + kBlock8 - 1) / kBlock8; }

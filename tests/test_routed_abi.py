@@ -113,8 +113,8 @@ def test_products():
     refused(g, [dict(N=0), dict(K=0), dict(rows=-1), dict(rows=513), dict(columns=500), dict(columns=0), dict(E=0),
                 dict(offsets=None), dict(dtype=3), dict(dW=None), dict(dW=P + 2), dict(Yt=None), dict(Ys=None),
                 dict(Xt=None), dict(Xs=None), dict(Yt=P + 8), dict(Xt=P + 1), dict(Ys=P + 1), dict(Xs=P + 2),
-                dict(columns=1 << 31)])
-    refused(g, [dict(E=1025), dict(N=(1 << 20) + 1), dict(K=(1 << 20) + 1)], UNSUPPORTED)
+                ])
+    refused(g, [dict(E=1025), dict(N=(1 << 20) + 1), dict(K=(1 << 20) + 1), dict(columns=(1 << 22) + 512)], UNSUPPORTED)
 
 
 def test_adamw():
