@@ -134,11 +134,16 @@ template <int BMT, bool PAIRED, bool EXACT> struct Worker {
 #pragma unroll
       for (int j = 0; j < G::TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  static __device__ __forceinline__ i32x8_t fragment(const uint8_t* rows, int row, int swizzle, int g) {
-    const u32x4_t lo = *(const u32x4_t*)(rows + row * kStep + (g ^ swizzle) * 16);
-    const u32x4_t hi = *(const u32x4_t*)(rows + row * kStep + ((g + 4) ^ swizzle) * 16);
+  // 16 bytes (16 k) of a row: chunk g for the step's first half of k, g + 4 for its second. (Which k
+  // of a block a lane has does not matter as long as both operands agree.)
+  static __device__ __forceinline__ u32x4_t chunk(const uint8_t* rows, int row, int swizzle, int c) {
+    return *(const u32x4_t*)(rows + row * kStep + (c ^ swizzle) * 16);
+  }
+  static __device__ __forceinline__ i32x8_t joined(u32x4_t lo, u32x4_t hi) {
     return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
   }
+  // Fragments are read ahead of the products that take them, so that the matrix cores do not wait for
+  // LDS; the scheduling barriers keep the reads where they are.
   __device__ __forceinline__ void step(const uint8_t* smem, int wm, int wn, int lane, int b, bool first) {
     const int x = lane & 15, g = lane >> 4;
     const uint8_t *As = smem + stage * G::STAGE, *Bs = As + G::A;
@@ -155,47 +160,66 @@ template <int BMT, bool PAIRED, bool EXACT> struct Worker {
 #pragma unroll
       for (int j = 0; j < G::TN; ++j) sb[j] >>= 8;
     }
+    const int arow = wm * (BMT / 2) + x, brow = wn * 64;
+    auto read_a = [&](int i, int h) { return chunk(As, arow + i * 16, x & 7, g + 4 * h); };
+    auto read_b = [&](int j, int h) {
+      const int row = brow + column_of<PAIRED>(j, x);
+      return chunk(Bs, row, swizzle_b<PAIRED>(row), g + 4 * h);
+    };
     if constexpr (EXACT) {
-      bf16x8_t bw[G::TN][4];
+      u32x4_t raw[G::TN], a = read_a(0, 0);
+      bf16x8_t bw[G::TN][2];
 #pragma unroll
-      for (int j = 0; j < G::TN; ++j) {
-        const int row = wn * 64 + column_of<PAIRED>(j, x);
-        const i32x8_t w = fragment(Bs, row, swizzle_b<PAIRED>(row), g);
-        const float by = scale8(sb[j] & 0xff);
+      for (int j = 0; j < G::TN; ++j) raw[j] = read_b(j, 0);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) bw[j][q] = decode8(w[2 * q], w[2 * q + 1], by);
-      }
-      __builtin_amdgcn_s_setprio(1);
+      for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int i = 0; i < G::TM; ++i) {
-        const int row = wm * (BMT / 2) + i * 16 + x;
-        const i32x8_t a = fragment(As, row, row & 7, g);
-        const float by = scale8(sa[i] & 0xff);
+        for (int j = 0; j < G::TN; ++j) {
+          const float by = scale8(sb[j] & 0xff);
+          bw[j][0] = decode8(raw[j][0], raw[j][1], by);
+          bw[j][1] = decode8(raw[j][2], raw[j][3], by);
+        }
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const bf16x8_t aw = decode8(a[2 * q], a[2 * q + 1], by);
+        for (int i = 0; i < G::TM; ++i) {
+          const u32x4_t now = a;
+          if (i + 1 < G::TM)
+            a = read_a(i + 1, h);
+          else if (h == 0)
+            a = read_a(0, 1);
+          if (h == 0 && i >= G::TM - 4) raw[i - (G::TM - 4)] = read_b(i - (G::TM - 4), 1);
+          __builtin_amdgcn_sched_barrier(0);
+          const float by = scale8(sa[i] & 0xff);
+          const bf16x8_t a0 = decode8(now[0], now[1], by), a1 = decode8(now[2], now[3], by);
 #pragma unroll
           for (int j = 0; j < G::TN; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[j][q], aw, acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[j][0], a0, acc[i][j], 0, 0, 0);
+#pragma unroll
+          for (int j = 0; j < G::TN; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[j][1], a1, acc[i][j], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
       }
-      __builtin_amdgcn_s_setprio(0);
     } else {
       i32x8_t bw[G::TN];
+      u32x4_t a[2] = {read_a(0, 0), read_a(0, 1)};
 #pragma unroll
-      for (int j = 0; j < G::TN; ++j) {
-        const int row = wn * 64 + column_of<PAIRED>(j, x);
-        bw[j] = fragment(Bs, row, swizzle_b<PAIRED>(row), g);
-      }
+      for (int j = 0; j < G::TN; ++j) bw[j] = joined(read_b(j, 0), read_b(j, 1));
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int i = 0; i < G::TM; ++i) {
-        const int row = wm * (BMT / 2) + i * 16 + x;
-        const i32x8_t a = fragment(As, row, row & 7, g);
+        const i32x8_t now = joined(a[0], a[1]);
+        if (i + 1 < G::TM) {
+          a[0] = read_a(i + 1, 0);
+          a[1] = read_a(i + 1, 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < G::TN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bw[j], a, acc[i][j], 0, 0, 0, (int)sb[j], 0,
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bw[j], now, acc[i][j], 0, 0, 0, (int)sb[j], 0,
                                                                        (int)sa[i]);
+        __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_s_setprio(0);
     }
@@ -220,7 +244,7 @@ template <int BMT, bool PAIRED, bool EXACT> struct Worker {
           __builtin_memcpy(&out, &acc[i][j], 16);
         }
         if (n + each <= w.n) {
-          store16(row + n, out);
+          __builtin_memcpy(row + n, &out, 16);
         } else {
           V v[each];
           __builtin_memcpy(v, &out, 16);
@@ -270,22 +294,25 @@ __global__ __launch_bounds__(kTileThreads) void k_product8_tiles(Product8 p) {
   count_units(p.offsets, p.E, rows, WEIGHTS ? kBlock8 : BMT, before);
   __syncthreads();
   const uint32_t tiles_n = (uint32_t)cdiv(WEIGHTS ? p.K : p.N, kTileN), each = (uint32_t)cdiv(p.N, BMT);
-  const uint32_t tiles_m = __builtin_amdgcn_readfirstlane(WEIGHTS ? p.E * each : (uint32_t)before[p.E]);
-  const uint32_t limit = (tiles_m * tiles_n + 7) / 8 * 8;
+  // the gradients go by one expert after the other, each dealt over all XCDs: their sums are as long as
+  // the experts' runs
+  const uint32_t tiles_m = __builtin_amdgcn_readfirstlane(WEIGHTS ? each : (uint32_t)before[p.E]);
+  const uint32_t turn = (tiles_m * tiles_n + 7) / 8 * 8, limit = WEIGHTS ? p.E * turn : turn;
   const int64_t ld = WEIGHTS ? p.columns : p.K, ls = WEIGHTS ? p.columns / kBlock8 : scale_row8(p.K);
   Loader<BMT, PAIRED> load(smem);
   const int lane = load.lane, wave = load.wave, wm = wave & 1, wn = wave >> 1;
 
   auto find = [&](uint32_t id, Where& w) {  // the tile at id or later of this workgroup's
-    uint32_t tm, tn;
-    for (; id < limit; id += gridDim.x)
-      if (tile_at(id, tiles_m, tiles_n, tm, tn)) break;
+    uint32_t e = 0, tm, tn;
+    for (; id < limit; id += gridDim.x) {
+      if (WEIGHTS) e = id / turn;
+      if (tile_at(id - e * turn, tiles_m, tiles_n, tm, tn)) break;
+    }
     if (id >= limit) return id;
     const uint8_t *A, *As, *B, *Bs;
     int bshift = 0;
     if constexpr (WEIGHTS) {
-      const uint32_t e = tm / each;
-      const int64_t m0 = (int64_t)(tm - e * each) * BMT, n0 = (int64_t)tn * kTileN;
+      const int64_t m0 = (int64_t)tm * BMT, n0 = (int64_t)tn * kTileN;
       const int b = before[e];
       w.m = (int)min((int64_t)BMT, p.N - m0);
       w.n = (int)min((int64_t)kTileN, p.K - n0);
@@ -295,7 +322,7 @@ __global__ __launch_bounds__(kTileThreads) void k_product8_tiles(Product8 p) {
       B = p.B + n0 * ld + (int64_t)b * kBlock8;
       As = p.As + m0 * ls + (b - w.b0);
       Bs = p.Bs + n0 * ls + (b - w.b0);
-      w.C = (char*)p.C + ((e * p.N + m0) * p.K + n0) * (int64_t)sizeof(V);
+      w.C = (char*)p.C + (((int64_t)e * p.N + m0) * p.K + n0) * (int64_t)sizeof(V);
       w.ldc = p.K;
     } else {
       int lo = 0, hi = p.E - 1;  // the last run with before[e] <= tm; it has units
@@ -306,8 +333,9 @@ __global__ __launch_bounds__(kTileThreads) void k_product8_tiles(Product8 p) {
         else
           hi = mid - 1;
       }
-      const int e = __builtin_amdgcn_readfirstlane(lo);
-      const int run = p.offsets ? offset8(p.offsets, e, rows) : 0, end = p.offsets ? offset8(p.offsets, e + 1, rows) : rows;
+      e = __builtin_amdgcn_readfirstlane(lo);
+      const int run = p.offsets ? offset8(p.offsets, (int)e, rows) : 0;
+      const int end = p.offsets ? offset8(p.offsets, (int)e + 1, rows) : rows;
       const int64_t m0 = run + (int64_t)((int)tm - before[e]) * BMT, n0 = (int64_t)tn * kTileN;
       w.m = (int)min((int64_t)BMT, end - m0);
       w.n = (int)min((int64_t)kTileN, p.N - n0);
@@ -315,8 +343,8 @@ __global__ __launch_bounds__(kTileThreads) void k_product8_tiles(Product8 p) {
       w.b0 = 0;
       A = p.A + m0 * ld;
       As = p.As + m0 * ls;
-      B = p.B + (e * p.N + n0) * ld;
-      Bs = p.Bs + (e * blocks8(p.N) + n0 / kBlock8) * ls;
+      B = p.B + ((int64_t)e * p.N + n0) * ld;
+      Bs = p.Bs + ((int64_t)e * blocks8(p.N) + n0 / kBlock8) * ls;
       bshift = 7;
       w.C = (char*)p.C + (m0 * p.N + n0) * (int64_t)sizeof(V);
       w.ldc = p.N;
@@ -456,8 +484,8 @@ __global__ __launch_bounds__(kStreamThreads) void k_product8_stream(Product8 p, 
 dim3 grid_of(int64_t tiles, int threads) { return dim3((unsigned)std::min<int64_t>(tiles, max_blocks(threads))); }
 
 template <int BMT, bool EXACT, bool WEIGHTS, typename V> hipError_t tiles(const Product8& p, int64_t count, hipStream_t s) {
-  if (count > INT32_MAX - 8) return hipErrorInvalidValue;  // of 2^15 results or more each: beyond any memory
-  const unsigned grid = (unsigned)std::min<int64_t>(up(count, 8), up(device_cus(), 8));
+  if (count > INT32_MAX - 8 * p.E) return hipErrorInvalidValue;  // of 2^15 results or more each: beyond any memory
+  const unsigned grid = (unsigned)std::min<int64_t>(up(count, 8), up(device_cus(), 8));  // 8: see tile_at
   hipLaunchKernelGGL((k_product8_tiles<BMT, EXACT, WEIGHTS, V>), dim3(grid), dim3(kTileThreads), 0, s, p);
   return hipGetLastError();
 }
