@@ -29,12 +29,11 @@ __device__ __forceinline__ float scale8(int byte) {
   return __uint_as_float(byte > 0 ? (uint32_t)byte << 23 : 1u << 22);
 }
 
-// Two codes in the lower bits: halves to even, NaN for what is not finite (the scaled magnitudes of
-// finite elements end at 448).
-__device__ __forceinline__ float finite8(float x) { return fabsf(x) < INFINITY ? x : NAN; }
+// Four codes: halves to even. The scaled magnitudes of finite elements end at 448; an infinity, which e4m3 does
+// not have, becomes NaN like a NaN.
 __device__ __forceinline__ uint32_t codes8(float a, float b, float c, float d) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(finite8(a), finite8(b), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(finite8(c), finite8(d), w, true);
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 
 // A unit of a run: `count` rows from `first` on, all of one expert; `index` units are before it in

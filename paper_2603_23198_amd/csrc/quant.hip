@@ -24,6 +24,25 @@ __device__ __forceinline__ uint32_t top16(uint32_t v) {
   return dpp_top<0x140>(v);
 }
 
+// Largest magnitude so far and of eight elements; a NaN has no part in it (fmaxf leaves it out), an infinity
+// has: where one shows, the caller counts again without those (see finite_top).
+__device__ __forceinline__ float most(float top, const float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+  return top;
+}
+__device__ __forceinline__ uint32_t finite_most(uint32_t top, const float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, magnitude8(x[i]));
+  return top;
+}
+// The bits of the largest finite magnitude of 16 lanes' eight elements each.
+__device__ __forceinline__ uint32_t top_of_row(const float (&x)[8]) {
+  uint32_t top = top16(__float_as_uint(most(0.f, x)));
+  if (top == 0x7f800000u) top = top16(finite_most(0u, x));
+  return top;
+}
+
 // Eight elements from column c on, zeros from column d on.
 template <typename V> __device__ __forceinline__ void load_eight(const V* row, int c, int d, float (&x)[8]) {
   if (c + 8 <= d) {
@@ -66,10 +85,7 @@ __global__ __launch_bounds__(kThreads) void k_quant_rows(const V* __restrict__ X
     if (t < t0 || t >= t1) continue;
     float x[8];
     load_eight(X + t * d, where ? where + t * d : nullptr, c, d, x);
-    uint32_t top = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, magnitude8(x[j]));
-    const int byte = scale_byte8(top16(top));
+    const int byte = scale_byte8(top_of_row(x));
     const float by = inverse8(byte);
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] *= by;
@@ -80,6 +96,43 @@ __global__ __launch_bounds__(kThreads) void k_quant_rows(const V* __restrict__ X
     const uint32_t four = (uint32_t)readlane_i(byte, 0) | (uint32_t)readlane_i(byte, 16) << 8 |
                           (uint32_t)readlane_i(byte, 32) << 16 | (uint32_t)readlane_i(byte, 48) << 24;
     if (lane == 0) *(uint32_t*)(S + t * sq + u * 4) = four;
+  }
+}
+
+// Eight neighbouring elements as they are in memory, and with those dropped where another eight are not above
+// zero.
+__device__ __forceinline__ void load_raw8(const bf16_t* p, Vec8<bf16_t>& v) { v.w = load16<u32x4_t>(p); }
+__device__ __forceinline__ void load_raw8(const float* p, Vec8<float>& v) {
+  v.a = load16<f32x4_t>(p);
+  v.b = load16<f32x4_t>(p + 4);
+}
+__device__ __forceinline__ void set(Vec8<bf16_t>& v, int i, bf16_t x) {
+  v.w[i / 2] = i & 1 ? (v.w[i / 2] & 0xffffu) | (uint32_t)x << 16 : (v.w[i / 2] & 0xffff0000u) | x;
+}
+__device__ __forceinline__ void set(Vec8<float>& v, int i, float x) {
+  if (i < 4)
+    v.a[i] = x;
+  else
+    v.b[i - 4] = x;
+}
+template <typename V> __device__ __forceinline__ void keep_where(Vec8<V>& v, const Vec8<V>& w) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (!(w.get(i) > 0.f)) set(v, i, V(0));
+}
+// The same of a row of d with zeros behind it, rows of fewer than eight element by element.
+template <typename V> __device__ __forceinline__ void load_edge(const V* row, int c, int d, Vec8<V>& v) {
+  if (d >= 8) {
+    v = load8(row, Cols{c, c + 4}, d);
+    return;
+  }
+  v = Vec8<V>{};
+#pragma unroll 1
+  for (int i = 0; i < 8; ++i) {
+    const V e = c + i < d ? row[c + i] : V(0);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k == i) set(v, k, e);
   }
 }
 
@@ -95,6 +148,21 @@ struct TileArgs {
   int64_t ldt, lds;        // row strides of Qt and St
   int E;
 };
+
+// Scale `at` of a row of n, and 127 up to `room` by the last one's writer.
+__device__ __forceinline__ void store_scale(uint8_t* S, int at, int n, int room, int byte) {
+  S[at] = (uint8_t)byte;
+  if (at == n - 1)
+    for (int s = n; s < room; ++s) S[s] = 127;
+}
+// A row's eight elements from column c0 on as codes.
+__device__ __forceinline__ void store_codes(const TileArgs& a, int64_t row, int c0, int tile, int tiles, int Cq, int sq,
+                                            int byte, const float (&v)[8], bool scale) {
+  const float by = inverse8(byte);
+  const u32x2_t w{codes8(v[0] * by, v[1] * by, v[2] * by, v[3] * by), codes8(v[4] * by, v[5] * by, v[6] * by, v[7] * by)};
+  __builtin_memcpy(a.Q + row * Cq + c0, &w, 8);
+  if (scale) store_scale(a.S + row * sq, tile, tiles, sq, byte);
+}
 
 // 128 rows x 128 columns per workgroup: thread (r, c) holds rows 8 r .. 8 r + 7 at columns 8 c ..
 // 8 c + 7, so that a load of 16 lanes is a run of 128 elements of a row, and the eight tokens of a
@@ -126,108 +194,122 @@ __global__ __launch_bounds__(kThreads) void k_quant_tile(TileArgs a) {
     }
     const V* X = (const V*)a.X + (matrix * R + row0) * C;
     const V* where = a.where ? (const V*)a.where + (int64_t)row0 * C : nullptr;
-    float x[8][8];
+    const int live = min(kBlock8, C - tile * kBlock8);
+    Vec8<V> x[8];
+    auto row_of = [&](int i) { return (int64_t)min(r * 8 + i, count - 1) * C; };
+    if (live == kBlock8) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t t = r * 8 + i;
-      if (t < count) {
-        load_eight(X + t * C, where ? where + t * C : nullptr, c0, C, x[i]);
-      } else {
+      for (int i = 0; i < 8; ++i) load_raw8(X + row_of(i) + c0, x[i]);
+      if (where) {
+        Vec8<V> w[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[i][j] = 0.f;
+        for (int i = 0; i < 8; ++i) load_raw8(where + row_of(i) + c0, w[i]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) keep_where(x[i], w[i]);
       }
-    }
-    // largest magnitudes of the columns over this wave's 32 rows, then over all
-    uint32_t col[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      col[j] = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) col[j] = max(col[j], magnitude8(x[i][j]));
-      col[j] = max(col[j], (uint32_t)__shfl_xor((int)col[j], 16, 64));
-      col[j] = max(col[j], (uint32_t)__shfl_xor((int)col[j], 32, 64));
-      if (SQUARE && j) col[0] = max(col[0], col[j]);
-    }
-    if (SQUARE) {
-      const uint32_t top = top16(col[0]);
-      if (lane == 0) top_of[wave][0] = top;
-    } else if (lane < 16) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top_of[wave][c * 8 + j] = col[j];
-    }
-    __syncthreads();
-    int byte[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (SQUARE && j) {
-        byte[j] = byte[0];
-        continue;
-      }
-      const int q = SQUARE ? 0 : c * 8 + j;
-      byte[j] = scale_byte8(max(max(top_of[0][q], top_of[1][q]), max(top_of[2][q], top_of[3][q])));
-    }
-    if (a.Q) {
+    } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        int b = byte[0];
-        if (!SQUARE) {
-          uint32_t top = 0;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) top = max(top, magnitude8(x[i][j]));
-          b = scale_byte8(top16(top));
+        load_edge(X + row_of(i), c0, C, x[i]);
+        if (where) {
+          Vec8<V> w;
+          load_edge(where + row_of(i), c0, C, w);
+          keep_where(x[i], w);
         }
-        const int t = r * 8 + i;
-        if (t < count) {
-          const float by = inverse8(b);
-          const u32x2_t w{codes8(x[i][0] * by, x[i][1] * by, x[i][2] * by, x[i][3] * by),
-                          codes8(x[i][4] * by, x[i][5] * by, x[i][6] * by, x[i][7] * by)};
-          const int64_t row = matrix * R + row0 + t;
-          __builtin_memcpy(a.Q + row * Cq + c0, &w, 8);
-          if (!SQUARE && c == 0) {
-            a.S[row * sq + tile] = (uint8_t)b;
-            if (tile == tiles - 1)
-              for (int s = tiles; s < sq; ++s) a.S[row * sq + s] = 127;
-          }
-        }
-      }
-      if (SQUARE && threadIdx.x == 0) {
-        uint8_t* S = a.S + (matrix * blocks8(R) + at) * sq;
-        S[tile] = (uint8_t)byte[0];
-        if (tile == tiles - 1)
-          for (int s = tiles; s < sq; ++s) S[s] = 127;
       }
     }
-    if (a.Qt) {
+    if (count < kBlock8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r * 8 + i >= count) x[i] = Vec8<V>{};
+    }
+    // Rows: their scales and codes; and the columns' largest magnitudes over this thread's rows. (The scheduling
+    // barriers keep one row's or column's values alive at a time: without them all 64 are, at 240 registers.)
+    uint32_t col[8] = {};
+    float high[8] = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float by = inverse8(byte[j]);
-        const u32x2_t w{codes8(x[0][j] * by, x[1][j] * by, x[2][j] * by, x[3][j] * by),
-                        codes8(x[4][j] * by, x[5][j] * by, x[6][j] * by, x[7][j] * by)};
-        __builtin_memcpy(&turned[(c * 8 + j) * kRow + r * 8], &w, 8);
+        v[j] = x[i].get(j);
+        high[j] = fmaxf(high[j], fabsf(v[j]));
+      }
+      if (!SQUARE && a.Q) {
+        const int t = r * 8 + i, b = scale_byte8(top_of_row(v));
+        if (t < count) store_codes(a, row0 + t, c0, tile, tiles, Cq, sq, b, v, c == 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    bool infinite = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      col[j] = __float_as_uint(high[j]);
+      infinite |= high[j] == INFINITY;
+    }
+    if (ballot(infinite)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        col[j] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) col[j] = max(col[j], magnitude8(x[i].get(j)));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (SQUARE) {
+#pragma unroll
+      for (int j = 1; j < 8; ++j) col[0] = max(col[0], col[j]);
+      col[0] = top16(col[0]);
+    }
+    // over the wave's 32 rows, then over all
+    if (SQUARE || a.Qt) {
+#pragma unroll
+      for (int j = 0; j < (SQUARE ? 1 : 8); ++j) {
+        col[j] = max(col[j], (uint32_t)__shfl_xor((int)col[j], 16, 64));
+        col[j] = max(col[j], (uint32_t)__shfl_xor((int)col[j], 32, 64));
+        if (lane < 16) top_of[wave][SQUARE ? 0 : c * 8 + j] = col[j];
       }
       __syncthreads();
-      const int live = min(kBlock8, C - tile * kBlock8);
-      uint8_t* Qt = a.Qt + (matrix * C + tile * kBlock8) * a.ldt + (int64_t)at * kBlock8;
+      auto byte_of = [&](int j) {
+        const int q = SQUARE ? 0 : c * 8 + j;
+        return scale_byte8(max(max(top_of[0][q], top_of[1][q]), max(top_of[2][q], top_of[3][q])));
+      };
+      const int one = SQUARE ? byte_of(0) : 0;
+      if (SQUARE && a.Q) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int n = i * 32 + threadIdx.x / 8, k = threadIdx.x % 8 * 16;
-        if (n < live) {
-          u32x4_t w;
-          __builtin_memcpy(&w, &turned[n * kRow + k], 16);
-          *(u32x4_t*)(Qt + n * a.ldt + k) = w;
+        for (int i = 0; i < 8; ++i) {
+          float v[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = x[i].get(j);
+          if (r * 8 + i < count) store_codes(a, matrix * R + row0 + r * 8 + i, c0, tile, tiles, Cq, sq, one, v, false);
+          __builtin_amdgcn_sched_barrier(0);
         }
+        if (threadIdx.x == 0) store_scale(a.S + (matrix * blocks8(R) + at) * sq, tile, tiles, sq, one);
       }
-      if (SQUARE) {
-        if (threadIdx.x == 0) {
-          uint8_t* St = a.St + (matrix * tiles + tile) * a.lds;
-          St[at] = (uint8_t)byte[0];
-          if (at == (int)blocks8(R) - 1)
-            for (int64_t s = at + 1; s < a.lds; ++s) St[s] = 127;
-        }
-      } else if (r == 0) {
+      if (a.Qt) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c0 + j < C) a.St[(int64_t)(c0 + j) * a.lds + at] = (uint8_t)byte[j];
+        for (int j = 0; j < 8; ++j) {
+          const int b = SQUARE ? one : byte_of(j);
+          const float by = inverse8(b);
+          const u32x2_t w{codes8(x[0].get(j) * by, x[1].get(j) * by, x[2].get(j) * by, x[3].get(j) * by),
+                          codes8(x[4].get(j) * by, x[5].get(j) * by, x[6].get(j) * by, x[7].get(j) * by)};
+          __builtin_memcpy(&turned[(c * 8 + j) * kRow + r * 8], &w, 8);
+          if (!SQUARE && r == 0 && c0 + j < C) a.St[(int64_t)(c0 + j) * a.lds + at] = (uint8_t)b;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        __syncthreads();
+        uint8_t* Qt = a.Qt + (matrix * C + tile * kBlock8) * a.ldt + (int64_t)at * kBlock8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int n = i * 32 + threadIdx.x / 8, k = threadIdx.x % 8 * 16;
+          if (n < live) {
+            u32x4_t w;
+            __builtin_memcpy(&w, &turned[n * kRow + k], 16);
+            *(u32x4_t*)(Qt + n * a.ldt + k) = w;
+          }
+        }
+        if (SQUARE && threadIdx.x == 0)
+          store_scale(a.St + (matrix * tiles + tile) * a.lds, at, (int)blocks8(R), (int)a.lds, one);
       }
     }
     __syncthreads();
