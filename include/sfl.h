@@ -805,8 +805,8 @@ typedef struct {
  * m keeps and the upper 16 below that of sqrt(v), and what is below is cut off. A root above zero never becomes
  * zero. Moments that are not finite are held as NaN, and no others.
  * Errors: SFL_E_ARG for n < 0, a NULL list (n > 0), cfg or step, a NULL buffer of a tensor with elements, scales
- * missing or given for fp32 moments, an unknown type, a half of bf16 parameters, betas outside [0, 1), eps not
- * above 0, lr, weight_decay or max_norm negative or NaN, norm without sumsq. */
+ * missing or given for fp32 moments, an unknown type, a half of bf16 parameters, betas outside [0, 1), eps below
+ * the normal fp32 numbers, lr, weight_decay or max_norm negative or NaN, norm without sumsq. */
 typedef struct {
   double lr, beta1, beta2, eps; /* 1 - beta is formed in 64 bits */
   double max_norm;              /* not read without sumsq */

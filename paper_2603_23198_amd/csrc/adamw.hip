@@ -102,11 +102,16 @@ __device__ __forceinline__ void decode(uint32_t w, float by, float (&x)[kUnit]) 
   x[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * by;
 }
 
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_top(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false));
+}
 // Largest value over aligned groups of 32 lanes.
 __device__ __forceinline__ uint32_t top32(uint32_t v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
-  return v;
+  v = dpp_top<0xB1>(v);
+  v = dpp_top<0x4E>(v);
+  v = dpp_top<0x141>(v);
+  v = dpp_top<0x140>(v);
+  return max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
 }
 
 // A scaled magnitude (at most 448) to e4m3's numbers, by 16 bits of noise; exact in e4m3. From 2^-6 on
@@ -124,10 +129,17 @@ __device__ __forceinline__ float drawn(float a, uint32_t noise, bool least) {
 }
 // Four elements to codes; the scale byte is that of the 32 lanes' 128 elements.
 __device__ __forceinline__ uint32_t encode(const float (&x)[kUnit], const uint32_t (&noise)[kUnit], bool least, int* byte) {
-  uint32_t top = 0;
+  float most = 0.f;  // a NaN has no part in it
 #pragma unroll
-  for (int j = 0; j < kUnit; ++j) top = max(top, magnitude8(x[j]));
-  *byte = scale_byte8(top32(top));
+  for (int j = 0; j < kUnit; ++j) most = fmaxf(most, fabsf(x[j]));
+  uint32_t top = top32(__float_as_uint(most));
+  if (top == 0x7f800000u) {  // an infinity: once more without those
+    top = 0;
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j) top = max(top, magnitude8(x[j]));
+    top = top32(top);
+  }
+  *byte = scale_byte8(top);
   const float by = inverse8(*byte);
   float q[kUnit];
 #pragma unroll
@@ -139,19 +151,22 @@ __device__ __forceinline__ uint32_t encode(const float (&x)[kUnit], const uint32
 }
 
 struct Now {  // of this step
-  float lr, inv1, inv2;
+  float lr, inv1, inv2;  // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
   uint32_t key;
 };
 
-// The new moments and parameter of one element. The moments round after every operation, as any
-// 32-bit form of the formulas does.
-__device__ __forceinline__ void advance(const Hyper& h, const Now& now, const Scale& clip, float decay, float grad,
-                                        float& p, float& m, float& v) {
+// The new moments and parameter of one element, and the root of the second moment, which is rounded to nearest
+// (moments in 8 bits hang on it). The moments round after every operation, as any 32-bit form of the formulas
+// does; the quotient takes the hardware's reciprocal (one last place off; its share of the parameter is lr).
+__device__ __forceinline__ float advance(const Hyper& h, const Now& now, const Scale& clip, float decay, float grad,
+                                         float& p, float& m, float& v) {
 #pragma clang fp contract(off)
   const float g = clip(grad);
   m = h.beta1 * m + h.rest1 * g;
   v = h.beta2 * v + h.rest2 * (g * g);
-  p = p - now.lr * (m * now.inv1 / (sqrtf(v * now.inv2) + h.eps) + decay * p);
+  const float root = sqrtf(v);
+  p = p - now.lr * (m * now.inv1 * __builtin_amdgcn_rcpf(root * now.inv2 + h.eps) + decay * p);
+  return root;
 }
 
 template <typename P, typename G, bool SMALL>
@@ -185,18 +200,22 @@ __device__ __forceinline__ void share(const sfl_adamw_t& t, uint64_t place, int6
       for (int j = 0; j < kUnit; ++j) v[s][j] *= v[s][j];
     }
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) advance(h, now, clip, t.weight_decay, g[s][j], p[s][j], m[s][j], v[s][j]);
+    for (int j = 0; j < kUnit; ++j) {
+      const float root = advance(h, now, clip, t.weight_decay, g[s][j], p[s][j], m[s][j], v[s][j]);
+      if (SMALL) v[s][j] = root;
+    }
     store_unit4((P*)t.param, i, t.n, p[s]);
     if (t.half) store_unit4((bf16_t*)t.half, i, t.n, p[s]);
     if (SMALL) {
+      // the four elements' places share their upper half: they begin at a multiple of four
       uint32_t low[kUnit], high[kUnit];
+      const uint64_t at_list = place + (uint64_t)i;
+      const uint32_t key = mix(now.key + (uint32_t)(at_list >> 32));
 #pragma unroll
       for (int j = 0; j < kUnit; ++j) {
-        const uint64_t at_list = place + (uint64_t)(i + j);
-        const uint32_t bits = mix(mix(now.key + (uint32_t)(at_list >> 32)) ^ (uint32_t)at_list);
+        const uint32_t bits = mix(key ^ ((uint32_t)at_list + j));
         low[j] = bits & 0xffffu;
         high[j] = bits >> 16;
-        v[s][j] = sqrtf(v[s][j]);
       }
       // lanes past the end have zeros: no part in a block's largest
       int byte_m, byte_v;
@@ -224,7 +243,7 @@ template <int MAX> __global__ __launch_bounds__(kThreads) void k_adamw(List<MAX>
     const double t = (double)(step > 1 ? step : 1);
     shared.lr = h.lr_scale ? h.lr * *h.lr_scale : h.lr;
     shared.inv1 = (float)(-1.0 / expm1(t * h.log_beta1));
-    shared.inv2 = (float)(-1.0 / expm1(t * h.log_beta2));
+    shared.inv2 = (float)sqrt(-1.0 / expm1(t * h.log_beta2));
     shared.key = mix((uint32_t)(step > 1 ? step : 1) + mix(h.seed));
   }
   __syncthreads();

@@ -3,6 +3,7 @@
 // route_groups.hip, quant.hip, product8.hip and adamw.hip.
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
 #include <cmath>
 
 #include "routed.h"
@@ -116,7 +117,7 @@ sfl_status_t sfl_quant_product_weights(const uint8_t* Yt, const uint8_t* Ys, int
 sfl_status_t sfl_adamw_step(const sfl_adamw_t* list, int32_t n, const sfl_adamw_cfg_t* cfg, sfl_stream_t stream) {
   if (n < 0 || (n > 0 && !list) || !cfg || !cfg->step) return SFL_E_ARG;
   auto beta_ok = [](double b) { return b >= 0.0 && b < 1.0; };
-  if (!beta_ok(cfg->beta1) || !beta_ok(cfg->beta2) || !(cfg->lr >= 0.0) || !((float)cfg->eps > 0.f) ||
+  if (!beta_ok(cfg->beta1) || !beta_ok(cfg->beta2) || !(cfg->lr >= 0.0) || !((float)cfg->eps >= FLT_MIN) ||
       (cfg->sumsq && !(cfg->max_norm >= 0.0)) || (cfg->norm && !cfg->sumsq))
     return SFL_E_ARG;
   for (int32_t i = 0; i < n; ++i) {
