@@ -51,8 +51,9 @@ __device__ __forceinline__ uint32_t mix(uint32_t h) {  // MurmurHash3's 32-bit f
   return h ^ (h >> 16);
 }
 
-template <typename V> __device__ __forceinline__ void load_unit4(const V* p, int64_t i, int64_t n, float (&x)[kUnit]) {
-  if (i + kUnit <= n) {
+// Four elements from i on, of n; ALL: all are there.
+template <bool ALL, typename V> __device__ __forceinline__ void load_unit4(const V* p, int64_t i, int64_t n, float (&x)[kUnit]) {
+  if (ALL || i + kUnit <= n) {
     V v[kUnit];
     __builtin_memcpy(v, p + i, sizeof(v));
 #pragma unroll
@@ -62,22 +63,29 @@ template <typename V> __device__ __forceinline__ void load_unit4(const V* p, int
     for (int j = 0; j < kUnit; ++j) x[j] = i + j < n ? VT<V>::load(p, i + j) : 0.f;
   }
 }
-template <typename V> __device__ __forceinline__ void store_unit4(V* p, int64_t i, int64_t n, const float (&x)[kUnit]) {
-  if (i + kUnit <= n) {
-    V v[kUnit];
+__device__ __forceinline__ void pack(const float (&x)[kUnit], float (&v)[kUnit]) {
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) v[j] = VT<V>::cvt(x[j]);
+  for (int j = 0; j < kUnit; ++j) v[j] = x[j];
+}
+__device__ __forceinline__ void pack(const float (&x)[kUnit], bf16_t (&v)[kUnit]) {
+  const u32x2_t w{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+  __builtin_memcpy(v, &w, 8);
+}
+template <bool ALL, typename V> __device__ __forceinline__ void store_unit4(V* p, int64_t i, int64_t n, const float (&x)[kUnit]) {
+  V v[kUnit];
+  pack(x, v);
+  if (ALL || i + kUnit <= n) {
     __builtin_memcpy(p + i, v, sizeof(v));
   } else {
 #pragma unroll
     for (int j = 0; j < kUnit; ++j)
-      if (i + j < n) VT<V>::store(p, i + j, x[j]);
+      if (i + j < n) p[i + j] = v[j];
   }
 }
 
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int64_t i, int64_t n) {
+template <bool ALL> __device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int64_t i, int64_t n) {
   uint32_t w = 0;
-  if (i + kUnit <= n) {
+  if (ALL || i + kUnit <= n) {
     __builtin_memcpy(&w, p + i, 4);
   } else {
 #pragma unroll
@@ -86,8 +94,8 @@ __device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int64_t i, int6
   }
   return w;
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, int64_t i, int64_t n, uint32_t w) {
-  if (i + kUnit <= n) {
+template <bool ALL> __device__ __forceinline__ void store_codes(uint8_t* p, int64_t i, int64_t n, uint32_t w) {
+  if (ALL || i + kUnit <= n) {
     __builtin_memcpy(p + i, &w, 4);
   } else {
 #pragma unroll
@@ -169,25 +177,25 @@ __device__ __forceinline__ float advance(const Hyper& h, const Now& now, const S
   return root;
 }
 
-template <typename P, typename G, bool SMALL>
-__device__ __forceinline__ void share(const sfl_adamw_t& t, uint64_t place, int64_t at, const Hyper& h, const Now& now,
-                                      const Scale& clip) {
+template <bool ALL, typename P, typename G, bool SMALL>
+__device__ __forceinline__ void turn(const sfl_adamw_t& t, uint64_t place, int64_t at, const Hyper& h, const Now& now,
+                                     const Scale& clip) {
   float p[kSteps][kUnit], g[kSteps][kUnit], m[kSteps][kUnit], v[kSteps][kUnit];
   uint32_t mq[kSteps], vq[kSteps];
   int mb[kSteps], vb[kSteps];
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
     const int64_t i = at + s * kStep + threadIdx.x * kUnit;
-    load_unit4((const P*)t.param, i, t.n, p[s]);
-    load_unit4((const G*)t.grad, i, t.n, g[s]);
+    load_unit4<ALL>((const P*)t.param, i, t.n, p[s]);
+    load_unit4<ALL>((const G*)t.grad, i, t.n, g[s]);
     if (SMALL) {
-      mq[s] = load_codes((const uint8_t*)t.m, i, t.n);
-      vq[s] = load_codes((const uint8_t*)t.v, i, t.n);
-      mb[s] = i < t.n ? t.m_scale[i / kBlock8] : 127;
-      vb[s] = i < t.n ? t.v_scale[i / kBlock8] : 127;
+      mq[s] = load_codes<ALL>((const uint8_t*)t.m, i, t.n);
+      vq[s] = load_codes<ALL>((const uint8_t*)t.v, i, t.n);
+      mb[s] = ALL || i < t.n ? t.m_scale[i / kBlock8] : 127;
+      vb[s] = ALL || i < t.n ? t.v_scale[i / kBlock8] : 127;
     } else {
-      load_unit4((const float*)t.m, i, t.n, m[s]);
-      load_unit4((const float*)t.v, i, t.n, v[s]);
+      load_unit4<ALL>((const float*)t.m, i, t.n, m[s]);
+      load_unit4<ALL>((const float*)t.v, i, t.n, v[s]);
     }
   }
 #pragma unroll
@@ -204,8 +212,8 @@ __device__ __forceinline__ void share(const sfl_adamw_t& t, uint64_t place, int6
       const float root = advance(h, now, clip, t.weight_decay, g[s][j], p[s][j], m[s][j], v[s][j]);
       if (SMALL) v[s][j] = root;
     }
-    store_unit4((P*)t.param, i, t.n, p[s]);
-    if (t.half) store_unit4((bf16_t*)t.half, i, t.n, p[s]);
+    store_unit4<ALL>((P*)t.param, i, t.n, p[s]);
+    if (t.half) store_unit4<ALL>((bf16_t*)t.half, i, t.n, p[s]);
     if (SMALL) {
       // the four elements' places share their upper half: they begin at a multiple of four
       uint32_t low[kUnit], high[kUnit];
@@ -220,17 +228,26 @@ __device__ __forceinline__ void share(const sfl_adamw_t& t, uint64_t place, int6
       // lanes past the end have zeros: no part in a block's largest
       int byte_m, byte_v;
       const uint32_t cm = encode(m[s], low, false, &byte_m), cv = encode(v[s], high, true, &byte_v);
-      store_codes((uint8_t*)t.m, i, t.n, cm);
-      store_codes((uint8_t*)t.v, i, t.n, cv);
-      if (i % kBlock8 == 0 && i < t.n) {
+      store_codes<ALL>((uint8_t*)t.m, i, t.n, cm);
+      store_codes<ALL>((uint8_t*)t.v, i, t.n, cv);
+      if (threadIdx.x % 32 == 0 && (ALL || i < t.n)) {
         t.m_scale[i / kBlock8] = (uint8_t)byte_m;
         t.v_scale[i / kBlock8] = (uint8_t)byte_v;
       }
     } else {
-      store_unit4((float*)t.m, i, t.n, m[s]);
-      store_unit4((float*)t.v, i, t.n, v[s]);
+      store_unit4<ALL>((float*)t.m, i, t.n, m[s]);
+      store_unit4<ALL>((float*)t.v, i, t.n, v[s]);
     }
   }
+}
+
+template <typename P, typename G, bool SMALL>
+__device__ __forceinline__ void share(const sfl_adamw_t& t, uint64_t place, int64_t at, const Hyper& h, const Now& now,
+                                      const Scale& clip) {
+  if (at + kShare <= t.n)
+    turn<true, P, G, SMALL>(t, place, at, h, now, clip);
+  else
+    turn<false, P, G, SMALL>(t, place, at, h, now, clip);
 }
 
 template <int MAX> __global__ __launch_bounds__(kThreads) void k_adamw(List<MAX> l, Hyper h) {
@@ -257,7 +274,7 @@ template <int MAX> __global__ __launch_bounds__(kThreads) void k_adamw(List<MAX>
     else
       hi = mid - 1;
   }
-  const sfl_adamw_t& t = l.t[lo];
+  const sfl_adamw_t t = l.t[lo];  // in registers: the stores below may not change it
   const int64_t at = (int64_t)((int)blockIdx.x - l.first[lo]) * kShare;
   const uint64_t place = l.place[lo];
   const int kind = (t.param_dtype == SFL_BF16 ? 4 : 0) | (t.grad_dtype == SFL_BF16 ? 2 : 0) | (t.moments ? 1 : 0);
