@@ -710,7 +710,7 @@ sfl_status_t sfl_route_groups_backward(const sfl_route_groups_bwd_args_t* args, 
  *           1). Tokens in no run are in no column, and their rows of Q and S are left as they are.
  *           Offsets that descend or pass T give codes without meaning (never an access out of bounds).
  * Errors: SFL_E_ARG for bad sizes, NULL or misaligned buffers, neither rows nor columns; SFL_E_UNSUPPORTED for
- * E > 1024, T > 2^31 - 1 - 128 E or d > 2^20. */
+ * E > 1024, T > 2^31 - 1 - 128 (E + 4), (T / 128 + 1) E > 2^31 - 1 or d > 2^20. */
 typedef struct {
   sfl_dtype_t dtype;
   int32_t E;
@@ -744,7 +744,7 @@ sfl_status_t sfl_quant_weights(const void* W, sfl_dtype_t dtype, int64_t E, int6
  *  Y        [rows][N] dtype (F32 or BF16); rows of no expert are left as they are
  * Results below the normal fp32 numbers may be zero. The sums' order depends on the sizes and not on the
  * rows' places. Errors: SFL_E_ARG for bad sizes, NULL or misaligned buffers; SFL_E_UNSUPPORTED for
- * E > 1024, rows or N > 2^31 - 1 - 128 E or K > 2^20. */
+ * E > 1024, rows or N > 2^31 - 1 - 128 (E + 4), (rows / 128 + 1) E > 2^31 - 1 or K > 2^20. */
 sfl_status_t sfl_quant_product(const uint8_t* Q, const uint8_t* S, int64_t rows, int64_t K, const uint8_t* W,
                                const uint8_t* Ws, int32_t E, int64_t N, const int32_t* offsets, sfl_dtype_t dtype,
                                void* Y, sfl_stream_t stream);

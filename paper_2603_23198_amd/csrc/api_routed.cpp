@@ -27,7 +27,9 @@ sfl_status_t check_scores(int32_t dtype, int32_t score, int64_t T, int32_t E, in
 // Tokens of E experts in runs: their columns and units are counted in 31 bits.
 sfl_status_t check_runs(int64_t T, int64_t E) {
   if (T < 0 || E < 1) return SFL_E_ARG;
-  return E > kMaxExperts8 || T > INT32_MAX - (int64_t)kBlock8 * (E + 4) ? SFL_E_UNSUPPORTED : SFL_OK;
+  if (E > kMaxExperts8 || T > INT32_MAX - (int64_t)kBlock8 * (E + 4)) return SFL_E_UNSUPPORTED;
+  // also runs that overlap, which no meaningful offsets make, are counted without overflow
+  return (T / kBlock8 + 1) * E > INT32_MAX ? SFL_E_UNSUPPORTED : SFL_OK;
 }
 
 // Codes and their scales: both or neither, aligned.

@@ -58,19 +58,20 @@ __device__ __forceinline__ Unit unit_of(const int32_t* __restrict__ offsets, int
     return u;
   }
   const int lane = lane_id(), per = (E + kWave - 1) / kWave, e0 = min(lane * per, E), e1 = min(e0 + per, E);
-  int mine = 0, at = offset8(offsets, e0, rows);
+  const int first0 = offset8(offsets, e0, rows);
+  int mine = 0, at = first0, end0 = first0;  // the lane's first run is first0 .. end0
   for (int e = e0; e < e1; ++e) {
     const int end = offset8(offsets, e + 1, rows);
     mine += (max(end - at, 0) + size - 1) / size;
+    if (e == e0) end0 = end;
     at = end;
   }
   const int incl = wave_incl_scan(mine);
   const uint64_t past = ballot(incl > index);
   if (past == 0) return u;
   const int l = __builtin_ctzll(past);
-  int before = readlane_i(incl - mine, l);
-  for (int e = l * per; e < E; ++e) {
-    const int first = offset8(offsets, e, rows), end = offset8(offsets, e + 1, rows);
+  int before = readlane_i(incl - mine, l), first = readlane_i(first0, l), end = readlane_i(end0, l);
+  for (int e = l * per;;) {
     const int n = (max(end - first, 0) + size - 1) / size;
     if (index < before + n) {
       u.expert = e;
@@ -80,8 +81,10 @@ __device__ __forceinline__ Unit unit_of(const int32_t* __restrict__ offsets, int
       return u;
     }
     before += n;
+    if (++e >= E) return u;
+    first = end;
+    end = offset8(offsets, e + 1, rows);
   }
-  return u;
 }
 
 // Run e in units of `size` rows: its rows and the units before it, by one wave.

@@ -32,9 +32,17 @@ __device__ __forceinline__ void load_lds16(u32x4_t rsrc, uint32_t lds_off, uint3
                : "v"(voff), "s"(rsrc), "s"(soff), "{m0}"(lds_off)
                : "memory");
 }
-// The same for 4 bytes per lane.
-__device__ __forceinline__ void load_lds4(u32x4_t rsrc, uint32_t lds_off, uint32_t voff, uint32_t soff) {
-  asm volatile("buffer_load_dword %0, %1, %2 offen lds"
+// The same, and for 4 bytes per lane, where a scalar operand may have been written by a vector instruction right
+// before: the memory instruction may read it five wait states later at the earliest, and the compiler, which
+// does that for its own loads, does not look into inline assembly. (Spilled scalars come back by v_readlane.)
+__device__ __forceinline__ void load_lds16_settled(u32x4_t rsrc, uint32_t lds_off, uint32_t voff, uint32_t soff) {
+  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
+               :
+               : "v"(voff), "s"(rsrc), "s"(soff), "{m0}"(lds_off)
+               : "memory");
+}
+__device__ __forceinline__ void load_lds4_settled(u32x4_t rsrc, uint32_t lds_off, uint32_t voff, uint32_t soff) {
+  asm volatile("s_nop 4\n\tbuffer_load_dword %0, %1, %2 offen lds"
                :
                : "v"(voff), "s"(rsrc), "s"(soff), "{m0}"(lds_off)
                : "memory");

@@ -102,15 +102,15 @@ template <int BMT, bool PAIRED> struct Loader {
   __device__ __forceinline__ void issue(const Where& w, int kt) {
     const uint32_t at = lds + stage_in * G::STAGE, k = (uint32_t)kt * kStep;
 #pragma unroll
-    for (int q = 0; q < G::LA; ++q) load_lds16(w.ra, at + (wave * G::LA + q) * 1024, offa[q], k);
+    for (int q = 0; q < G::LA; ++q) load_lds16_settled(w.ra, at + (wave * G::LA + q) * 1024, offa[q], k);
 #pragma unroll
-    for (int q = 0; q < G::LB; ++q) load_lds16(w.rb, at + G::A + (wave * G::LB + q) * 1024, offb[q], k);
+    for (int q = 0; q < G::LB; ++q) load_lds16_settled(w.rb, at + G::A + (wave * G::LB + q) * 1024, offb[q], k);
     stage_in = stage_in == G::NS - 1 ? 0 : stage_in + 1;
     if (kt == 0 || ((w.b0 + kt) & 3) == 0) {
       // waves 0 .. BMT / 64 - 1 bring the rows' scales, waves 4 .. 7 the columns'
       const int first = wave < 4 ? wave * 64 : BMT + (wave - 4) * 64;
       if (wave >= 4 || wave * 64 < BMT)
-        load_lds4(w.rs, lds + G::NS * G::STAGE + word_in * G::WORDS + first * 4, w.offs, (uint32_t)((w.b0 + kt) >> 2) * 4);
+        load_lds4_settled(w.rs, lds + G::NS * G::STAGE + word_in * G::WORDS + first * 4, w.offs, (uint32_t)((w.b0 + kt) >> 2) * 4);
       word_in = (word_in + 1) & (kWordRing - 1);
     }
   }
@@ -395,88 +395,121 @@ __global__ __launch_bounds__(kTileThreads) void k_product8_tiles(Product8 p) {
 }
 
 // ---- few rows of an expert: its weights pass by once ---------------------------------------
-// A wave has 16 columns and up to 16 MT rows, its operands come from memory into registers: bound by the
-// weights' bytes, so the products are the exact ones in bf16. The KS waves that share columns have a part
-// of the blocks each and add their sums over LDS, in order; so few columns still fill the chip.
+// A wave has 16 columns and up to 16 MT rows. The weights come from memory into registers, the next ones
+// on their way while some are used: bound by their bytes, so the products are the exact ones in bf16. The
+// rows, which all waves of a workgroup need, lie in LDS in chunks of 1024 k (read by every wave from the L2,
+// they and their scales took as long as the weights: 64 rows of eight experts, 4096 x 4096, 45 us, without
+// them 27). The KS waves that share columns have a part of the blocks each and add their sums over LDS, in
+// order; so few columns still fill the chip.
 constexpr int kStreamThreads = 512, kStreamWaves = kStreamThreads / kWave;
 
 template <int MT, int KS, typename V>
 __global__ __launch_bounds__(kStreamThreads) void k_product8_stream(Product8 p, int64_t units) {
-  constexpr int STRIPS = kStreamWaves / KS, UNROLL = MT == 1 ? 4 : 2;
-  __shared__ f32x4_t part[KS > 1 ? kStreamWaves : 1][MT][kWave];
-  const int lane = lane_id(), wave = threadIdx.x / kWave, x = lane & 15, g = lane >> 4;
-  const int ks = wave % KS, strip = wave / KS, rows = (int)p.rows;
+  constexpr int STRIPS = kStreamWaves / KS, UNROLL = 2;
+  constexpr int CHUNK = 1024, BLOCKS = CHUNK / kBlock8, WORDS = BLOCKS / 4;  // of a row
+  constexpr int CODES = 16 * MT * CHUNK, LOADS = CODES / 1024 / kStreamWaves;
+  static_assert(BLOCKS % KS == 0 && 16 * MT * WORDS <= 2 * kWave && CODES >= kStreamWaves * MT * 1024, "");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[CODES + 512];
+  const int lane = lane_id(), x = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), ks = wave % KS, strip = wave / KS;
+  const int rows = (int)p.rows, blocks = (int)(p.K / kBlock8);
   const int64_t strips = cdiv(p.N, 16 * STRIPS), total = units * strips, sk = scale_row8(p.K);
-  const int blocks = (int)(p.K / kBlock8), k0 = (int)((int64_t)blocks * ks / KS), k1 = (int)((int64_t)blocks * (ks + 1) / KS);
+  const uint32_t lds = __builtin_amdgcn_readfirstlane(
+      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)smem);
   for (int64_t id = blockIdx.x; id < total; id += gridDim.x) {
     const int64_t unit = id / strips, n0 = ((id - unit * strips) * STRIPS + strip) * 16;
     const Unit u = unit_of(p.offsets, p.E, rows, 16 * MT, (int)unit);
     if (u.expert < 0) return;
-    const int64_t n = min(n0 + x, p.N - 1);
-    const uint8_t* B = p.B + (u.expert * p.N + n) * p.K + g * 16;
-    const uint8_t* Bs = p.Bs + (u.expert * blocks8(p.N) + n / kBlock8) * sk;
-    const uint8_t *A[MT], *As[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int64_t m = u.first + min(i * 16 + x, u.count - 1);
-      A[i] = p.A + m * p.K + g * 16;
-      As[i] = p.As + m * sk;
-    }
+    const int count = __builtin_amdgcn_readfirstlane(u.count), expert = __builtin_amdgcn_readfirstlane(u.expert);
+    const int64_t first = __builtin_amdgcn_readfirstlane(u.first), n = min(n0 + x, p.N - 1);
+    const uint8_t* B = p.B + (expert * p.N + n) * p.K + g * 16;
+    const uint32_t* Bs = (const uint32_t*)(p.Bs + (expert * blocks8(p.N) + min(n0, p.N - 1) / kBlock8) * sk);
+    const u32x4_t ra = buffer_of(p.A + first * p.K, count * p.K), rs = buffer_of(p.As + first * sk, count * sk);
     f32x4_t acc[MT] = {};
-    for (int b0 = k0; b0 < k1; b0 += UNROLL) {
-      u32x4_t w[UNROLL][2], a[UNROLL][MT][2];
-      int sb[UNROLL], sa[UNROLL][MT];
+    for (int c0 = 0; c0 < blocks; c0 += BLOCKS) {
+      // a load fills 1 KB of one row, eight blocks; chunk c of a block lies at position c ^ (row & 7)
 #pragma unroll
-      for (int q = 0; q < UNROLL; ++q) {
-        const int b = min(b0 + q, k1 - 1);
-        w[q][0] = *(const u32x4_t*)(B + (int64_t)b * kBlock8);
-        w[q][1] = *(const u32x4_t*)(B + (int64_t)b * kBlock8 + 64);
-        sb[q] = Bs[b];
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-          if (i * 16 < u.count) {
-            a[q][i][0] = *(const u32x4_t*)(A[i] + (int64_t)b * kBlock8);
-            a[q][i][1] = *(const u32x4_t*)(A[i] + (int64_t)b * kBlock8 + 64);
-            sa[q][i] = As[i][b];
-          }
+      for (int q = 0; q < LOADS; ++q) {
+        const int at = (wave * LOADS + q) * 1024, row = at / CHUNK, b = c0 + at % CHUNK / kBlock8 + lane / 8;
+        const bool there = row < count && b < blocks;
+        load_lds16_settled(ra, lds + at, there ? (uint32_t)row * (uint32_t)p.K + b * kBlock8 + ((lane & 7) ^ (row & 7)) * 16 : kOOB, 0);
       }
-#pragma unroll
-      for (int q = 0; q < UNROLL; ++q) {
-        if (b0 + q >= k1) break;
-        bf16x8_t bw[4];
-        const float by = scale8(sb[q]);
-#pragma unroll
-        for (int h = 0; h < 4; ++h) bw[h] = decode8(w[q][h / 2][h % 2 * 2], w[q][h / 2][h % 2 * 2 + 1], by);
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-          if (i * 16 < u.count) {
-            const float bya = scale8(sa[q][i]);
-#pragma unroll
-            for (int h = 0; h < 4; ++h)
-              acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                  bw[h], decode8(a[q][i][h / 2][h % 2 * 2], a[q][i][h / 2][h % 2 * 2 + 1], bya), acc[i], 0, 0, 0);
-          }
+      if (wave < 2) {
+        const int word = wave * 64 + lane, row = word / WORDS, b = c0 + word % WORDS * 4;
+        load_lds4_settled(rs, lds + CODES + wave * 256, row < count && b < blocks ? (uint32_t)row * (uint32_t)sk + b : kOOB, 0);
       }
+      u32x4_t w[UNROLL][2], next[UNROLL][2];
+      const int mine = (min(blocks - c0, BLOCKS) - ks + KS - 1) / KS;  // this wave's: c0 + ks, c0 + ks + KS, ...
+      auto fetch = [&](int i0, u32x4_t(&to)[UNROLL][2]) {
+#pragma unroll
+        for (int q = 0; q < UNROLL; ++q) {
+          const int b = min(c0 + ks + max(min(i0 + q, mine - 1), 0) * KS, blocks - 1);
+          const uint8_t* at = B + (int64_t)b * kBlock8;
+          to[q][0] = *(const u32x4_t*)at;
+          to[q][1] = *(const u32x4_t*)(at + 64);
+        }
+      };
+      fetch(0, w);
+      __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's loads into LDS have landed
+      __syncthreads();
+      for (int i0 = 0; i0 < mine; i0 += UNROLL) {
+        if (i0 + UNROLL < mine) fetch(i0 + UNROLL, next);
+#pragma unroll
+        for (int q = 0; q < UNROLL; ++q) {
+          if (i0 + q >= mine) break;
+          const int in = ks + (i0 + q) * KS, b = c0 + in;
+          const float by = scale8(Bs[b >> 2] >> (b & 3) * 8 & 0xff);
+          bf16x8_t bw[4];
+#pragma unroll
+          for (int h = 0; h < 4; ++h) bw[h] = decode8(w[q][h / 2][h % 2 * 2], w[q][h / 2][h % 2 * 2 + 1], by);
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+            if (i * 16 < count) {
+              const uint8_t* row = smem + (i * 16 + x) * CHUNK + in * kBlock8;
+              const u32x4_t a[2] = {*(const u32x4_t*)(row + (g ^ (x & 7)) * 16), *(const u32x4_t*)(row + ((g + 4) ^ (x & 7)) * 16)};
+              const float bya = scale8(smem[CODES + (i * 16 + x) * BLOCKS + in]);
+#pragma unroll
+              for (int h = 0; h < 4; ++h)
+                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    bw[h], decode8(a[h / 2][h % 2 * 2], a[h / 2][h % 2 * 2 + 1], bya), acc[i], 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < UNROLL; ++q) {
+          w[q][0] = next[q][0];
+          w[q][1] = next[q][1];
+        }
+      }
+      __syncthreads();  // the chunk's place is free again
     }
     if (KS > 1) {
+      f32x4_t* part = (f32x4_t*)smem;  // [wave][MT][lane]
 #pragma unroll
-      for (int i = 0; i < MT; ++i) part[wave][i][lane] = acc[i];
+      for (int i = 0; i < MT; ++i) part[(wave * MT + i) * kWave + lane] = acc[i];
       __syncthreads();
       if (ks == 0)
 #pragma unroll
         for (int i = 0; i < MT; ++i)
-          for (int q = 1; q < KS; ++q) acc[i] += part[wave + q][i][lane];
+          for (int q = 1; q < KS; ++q) acc[i] += part[((wave + q) * MT + i) * kWave + lane];
       __syncthreads();
     }
     if (ks == 0)
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         const int m = i * 16 + x;
-        if (m >= u.count) continue;
-        V* row = (V*)p.C + (u.first + m) * p.N;
+        const int64_t at = n0 + 4 * g;
+        if (m >= count || at >= p.N) continue;
+        V* to = (V*)p.C + (first + m) * p.N + at;
+        V v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (n0 + 4 * g + e < p.N) VT<V>::store(row, n0 + 4 * g + e, acc[i][e]);
+        for (int e = 0; e < 4; ++e) v[e] = VT<V>::cvt(acc[i][e]);
+        if (at + 4 <= p.N) {
+          __builtin_memcpy(to, v, sizeof(v));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (at + e < p.N) to[e] = v[e];
+        }
       }
   }
 }
@@ -509,9 +542,9 @@ int64_t most_units(const Product8& p, int64_t size) {
 hipError_t launch_product8(const Product8& p, int bf16, hipStream_t s) {
   const int64_t live = std::min<int64_t>(p.E, p.rows);
   if (p.rows <= 64 * live) {
-    const int64_t waves = live * cdiv(p.N, 16), want = (int64_t)device_cus() * 8;
+    const int64_t waves = live * cdiv(p.N, 16), want = (int64_t)device_cus() * 16;
     const int ks = waves * 8 <= want ? 8 : waves * 4 <= want ? 4 : waves * 2 <= want ? 2 : 1;
-    if (p.rows <= 16) {
+    if (p.rows <= 4 * live) {
       const int64_t units = most_units(p, 16);
       return ks == 8 ? stream<1, 8>(p, bf16, units, s) : ks == 4 ? stream<1, 4>(p, bf16, units, s)
            : ks == 2 ? stream<1, 2>(p, bf16, units, s) : stream<1, 1>(p, bf16, units, s);

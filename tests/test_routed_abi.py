@@ -114,6 +114,7 @@ def test_products():
                 dict(offsets=None), dict(dtype=3), dict(dW=None), dict(dW=P + 2), dict(Yt=None), dict(Ys=None),
                 dict(Xt=None), dict(Xs=None), dict(Yt=P + 8), dict(Xt=P + 1), dict(Ys=P + 1), dict(Xs=P + 2),
                 ])
+    refused(f, [dict(E=1024, rows=(1 << 28) + 128)], UNSUPPORTED)
     refused(g, [dict(E=1025), dict(N=(1 << 20) + 1), dict(K=(1 << 20) + 1), dict(columns=(1 << 22) + 512)], UNSUPPORTED)
 
 
