@@ -29,11 +29,11 @@ def assert_product(got, x, w, dt, name=""):
     if dt == "bf16":
         n = up(x.shape[1], 8)
         pad = ((0, 0), (0, n - x.shape[1]))
-        a, c = np.abs(np.pad(x, pad)).reshape(-1, n // 8, 8), np.abs(np.pad(w, pad)).reshape(-1, n // 8, 8)
-        largest = np.zeros_like(ref)
+        a, c = (torch.from_numpy(np.abs(np.pad(t, pad))).cuda().view(-1, n // 8, 8) for t in (x, w))
+        largest = torch.zeros(ref.shape, dtype=torch.float64, device="cuda")
         for g in range(n // 8):
-            largest += (a[:, None, g] * c[None, :, g]).max(2)
-        tol = tol + 8 * 2.0 ** -13 * largest
+            largest += (a[:, None, g] * c[None, :, g]).amax(2)
+        tol = tol + 8 * 2.0 ** -13 * largest.cpu().numpy()
         tol = tol + U_BF16 * (np.abs(ref) + tol)
     err = np.abs(got - ref)
     bad = ~(err <= tol + 1e-37)
@@ -258,3 +258,81 @@ def test_a_row_does_not_depend_on_its_place():
     b.sfl_quant_product(Q, S, W, Ws, out[0])
     b.sfl_quant_product(Q.view(torch.uint8)[turn].view(Q.dtype), S[turn], W, Ws, out[1])
     assert same_bits(out[0][turn], out[1])
+
+
+# Results of more than 768 K values in runs of more than 16 rows come from tiles: of 128 rows, from 512 rows a
+# run on of 256.
+LOW, HIGH = [130, 5, 0, 257, 31], [700, 513, 1, 900]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [128, 384, 512, 1152])
+@pytest.mark.parametrize("loads,N", [(LOW, 1901), (HIGH, 1000), (HIGH, 513), ([300] * 3, 2048)])
+def test_tiles_of_ragged_runs(dt, K, loads, N):
+    """One to nine steps (scale words of four, begun and not), rows and columns that end inside a tile."""
+    product(loads, K, N, dt, seed=K + N)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("loads,N", [(LOW, 1901), (HIGH, 800)])
+def test_tiles_leave_rows_of_no_expert(dt, loads, N):
+    product(loads, 256, N, dt, first=9, rows=sum(loads) + 50, kind="wide")
+
+
+def test_tiles_of_one_expert_without_offsets():
+    rng = np.random.default_rng(3)
+    for rows, N in ((260, 3100), (1030, 1025)):
+        Q, S, x = codes_on_gpu(*o.quant(operand(rng, rows, 384)))
+        W, Ws, w = codes_on_gpu(*o.quant_square(operand(rng, N, 384)), 128)
+        for dt in ("bf16", "f32"):
+            Y = Out((rows, N), DT[dt])
+            b.sfl_quant_product(Q, S, W, Ws, Y.t)
+            assert_product(Y.values(), x, w, dt)
+
+
+@pytest.mark.parametrize("rows,N", [(300, 2700), (900, 900)])
+def test_tiles_keep_numbers_that_are_not_finite_to_their_rows(rows, N):
+    rng = np.random.default_rng(5)
+    xc, xe = o.quant(operand(rng, rows, 256))
+    wc, we = o.quant_square(operand(rng, N, 256))
+    xc[rows - 1, 77], wc[N - 1, 200] = 127, 255
+    Q, S, x = codes_on_gpu(xc, xe)
+    W, Ws, w = codes_on_gpu(wc, we, 128)
+    for dt in ("bf16", "f32"):
+        Y = Out((rows, N), DT[dt])
+        b.sfl_quant_product(Q, S, W, Ws, Y.t)
+        got = Y.values()
+        want = np.zeros((rows, N), bool)
+        want[-1], want[:, -1] = True, True
+        np.testing.assert_array_equal(np.isnan(got), want)
+        assert_product(got[:-1, :-1], x[:-1], w[:-1], dt)
+
+
+def test_tiles_by_offsets_without_meaning_stay_in_bounds():
+    rng = np.random.default_rng(6)
+    T, N = 1000, 2000
+    Q, S, _ = codes_on_gpu(*o.quant(operand(rng, T, 256)))
+    W, Ws, _ = codes_on_gpu(*o.quant_square(operand(rng, 128 * 3, 256)), 128)
+    W = W.view(torch.uint8).view(3, 128, 256).repeat(1, 16, 1)[:, :N].contiguous().view(W.dtype)
+    Ws = Ws.view(3, 1, 4).repeat(1, 16, 1).contiguous()
+    for of in ([50, 20, 90, 10], [-5, 3000, 7, 1000], [0, T, 0, T], [1 << 30, -(1 << 30), 5, T]):
+        Y = Out((T, N), torch.bfloat16)
+        b.sfl_quant_product(Q, S, W, Ws, Y.t, offsets=torch.tensor(of, dtype=torch.int32, device="cuda"))
+        Y.values()
+
+
+def test_tiles_repeat_and_replay():
+    p = product(HIGH, 384, 1000, "bf16")
+    args, first = (p["Q"], p["S"], p["W"], p["Ws"]), p["Y"].t.clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        b.sfl_quant_product(*args, p["Y"].t, offsets=p["offsets"])
+    for loads in (HIGH, [1, 2000, 100, 13], [0, 0, 2114, 0], [1057, 0, 0, 1057]):
+        p["offsets"].copy_(run_offsets(loads)[1])
+        p["Y"].t.zero_()
+        b.sfl_quant_product(*args, p["Y"].t, offsets=p["offsets"])
+        want = p["Y"].t.clone()
+        p["Y"].t.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert same_bits(p["Y"].t, want) and (loads != HIGH or same_bits(want, first))
