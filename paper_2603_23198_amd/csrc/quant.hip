@@ -2,7 +2,8 @@
 // which its largest magnitude comes down to 448, and the nearest e4m3 codes of x 2^-e. Blocks lie
 // along a row (k_quant_rows), along a row and along a run's tokens at once, or in squares of 128 x 128
 // (k_quant_tile). Bound by memory: every element is read once for both layouts. 16384 x 4096 bf16: rows
-// 40 us (5.0 TB/s), both layouts 70 (3.8; 190 registers leave two waves a SIMD); 4096 x 16384 fp32 in squares, both
+// 40 us (5.0 TB/s), both layouts 64 (4.2; 158 registers, three waves a SIMD; with a tile's elements kept
+// unpacked 190, two waves and 70 us); 4096 x 16384 fp32 in squares, both
 // layouts, 80 us (5.1).
 #include "blocks8.h"
 #include "rows.h"
@@ -138,6 +139,11 @@ template <typename V> __device__ __forceinline__ void load_edge(const V* row, in
   }
 }
 
+// The packed elements, hidden from the optimiser, which would keep all of a tile's unpacked from one use of them to
+// the next.
+__device__ __forceinline__ void hide(Vec8<bf16_t>& v) { asm volatile("" : "+v"(v.w)); }
+__device__ __forceinline__ void hide(Vec8<float>&) {}
+
 struct TileArgs {
   const void* X;
   const void* where;
@@ -241,6 +247,7 @@ __global__ __launch_bounds__(kThreads) void k_quant_tile(TileArgs a) {
         const int t = r * 8 + i, b = scale_byte8(top_of_row(v));
         if (t < count) store_codes(a, row0 + t, c0, tile, tiles, Cq, sq, b, v, c == 0);
       }
+      hide(x[i]);
       __builtin_amdgcn_sched_barrier(0);
     }
     bool infinite = false;
