@@ -127,6 +127,7 @@ class Grad(Structure):
     _fields_ = [("src", c_void_p), ("dst", c_void_p), ("n", c_int64), ("dtype", c_int32), ("reserved", c_int32)]
 
 
+SFL_BF16_FAST = 0x101  # of the products' results
 SFL_SCORE_SIGMOID, SFL_SCORE_SOFTMAX = 0, 1
 SFL_MOMENTS_F32, SFL_MOMENTS_8BIT = 0, 1
 
@@ -632,21 +633,31 @@ def sfl_quant_weights(W, Q=None, S=None, *, Qt=None, St=None, stream=None):
                                   *_codes(Qt, St, E * C, r, E * (c // 128)), _stream(stream)))
 
 
-def sfl_quant_product(Q, S, W, Ws, Y, *, offsets=None, stream=None):
+def _result(dt, fast):
+    """The type of a product's result; fast: bf16 from the 8-bit matrix instruction, which drops what lies 13 bits
+    below the largest of eight neighbouring products."""
+    if fast and dt != SFL_BF16:
+        raise ValueError("fast products have bf16 results")
+    return SFL_BF16_FAST if fast else dt
+
+
+def sfl_quant_product(Q, S, W, Ws, Y, *, offsets=None, fast=False, stream=None):
     (rows, K), N, dt = Q.shape, W.shape[-2], dtype_code(Y.dtype)
+    result = _result(dt, fast)
     E = W.shape[0] if W.dim() == 3 else 1
     if offsets is not None and offsets.numel() != E + 1:
         raise ValueError(f"offsets of {E} experts are {E + 1}, got {offsets.numel()}")
     q, s = _codes(Q, S, rows, K, rows)
     w, ws = _codes(W, Ws, E * N, K, E * (_up(N, 128) // 128))
     _check("sfl_quant_product",
-           _lib.sfl_quant_product(q, s, rows, K, w, ws, E, N, _buf(offsets, _I32, E + 1), dt,
+           _lib.sfl_quant_product(q, s, rows, K, w, ws, E, N, _buf(offsets, _I32, E + 1), result,
                                   _buf(Y, dt, rows * N, N), _stream(stream)))
 
 
-def sfl_quant_product_weights(Yt, Ys, Xt, Xs, dW, *, rows=None, offsets=None, stream=None):
+def sfl_quant_product_weights(Yt, Ys, Xt, Xs, dW, *, rows=None, offsets=None, fast=False, stream=None):
     """rows: the tokens of the one run without offsets (with them, they say how many there are)."""
     (N, columns), K, dt = Yt.shape, Xt.shape[0], dtype_code(dW.dtype)
+    result = _result(dt, fast)
     E = 1 if offsets is None else offsets.numel() - 1
     if rows is None:
         if offsets is None:
@@ -655,8 +666,8 @@ def sfl_quant_product_weights(Yt, Ys, Xt, Xs, dW, *, rows=None, offsets=None, st
     yt, ys = _codes(Yt, Ys, N, columns, N)
     xt, xs = _codes(Xt, Xs, K, columns, K)
     _check("sfl_quant_product_weights",
-           _lib.sfl_quant_product_weights(yt, ys, N, xt, xs, K, rows, columns, _buf(offsets, _I32, E + 1), E, dt,
-                                          _buf(dW, dt, E * N * K, K), _stream(stream)))
+           _lib.sfl_quant_product_weights(yt, ys, N, xt, xs, K, rows, columns, _buf(offsets, _I32, E + 1), E,
+                                          result, _buf(dW, dt, E * N * K, K), _stream(stream)))
 
 
 def adamw_list(params, grads, m, v, *, halves=None, m_scales=None, v_scales=None, weight_decay=0.0):

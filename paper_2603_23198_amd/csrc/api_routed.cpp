@@ -13,6 +13,8 @@ using namespace sfl;
 namespace {
 
 bool dtype_ok(int32_t t) { return t == SFL_F32 || t == SFL_BF16; }
+bool result_ok(int32_t t) { return dtype_ok(t) || t == SFL_BF16_FAST; }  // of a product
+uintptr_t result_size(int32_t t) { return t == SFL_F32 ? 4 : 2; }
 bool aligned(const void* p, uintptr_t by) { return (uintptr_t)p % by == 0; }
 sfl_status_t status(hipError_t e) { return e == hipSuccess ? SFL_OK : SFL_E_HIP; }
 
@@ -90,15 +92,15 @@ sfl_status_t sfl_quant_product(const uint8_t* Q, const uint8_t* S, int64_t rows,
                                const uint8_t* Ws, int32_t E, int64_t N, const int32_t* offsets, sfl_dtype_t dtype,
                                void* Y, sfl_stream_t stream) {
   sfl_status_t st = check_runs(rows, E);
-  if (st == SFL_E_ARG || !dtype_ok(dtype) || K < kBlock8 || K % kBlock8 || N < 1 || (!offsets && E != 1))
+  if (st == SFL_E_ARG || !result_ok(dtype) || K < kBlock8 || K % kBlock8 || N < 1 || (!offsets && E != 1))
     return SFL_E_ARG;
   if (st != SFL_OK || K > kMaxWidth8 || N > INT32_MAX - (int64_t)kBlock8 * (E + 4)) return SFL_E_UNSUPPORTED;
-  if (!aligned(Q, 16) || !aligned(W, 16) || !aligned(S, 4) || !aligned(Ws, 4) || !aligned(Y, dtype == SFL_BF16 ? 2 : 4))
+  if (!aligned(Q, 16) || !aligned(W, 16) || !aligned(S, 4) || !aligned(Ws, 4) || !aligned(Y, result_size(dtype)))
     return SFL_E_ARG;
   if (rows == 0) return SFL_OK;
   if (!Q || !S || !W || !Ws || !Y) return SFL_E_ARG;
   const Product8 p{Q, S, W, Ws, Y, offsets, rows, N, K, 0, E};
-  return status(launch_product8(p, dtype == SFL_BF16, (hipStream_t)stream));
+  return status(launch_product8(p, dtype, (hipStream_t)stream));
 }
 
 sfl_status_t sfl_quant_product_weights(const uint8_t* Yt, const uint8_t* Ys, int64_t N, const uint8_t* Xt,
@@ -106,14 +108,14 @@ sfl_status_t sfl_quant_product_weights(const uint8_t* Yt, const uint8_t* Ys, int
                                        const int32_t* offsets, int32_t E, sfl_dtype_t dtype, void* dW,
                                        sfl_stream_t stream) {
   sfl_status_t st = check_runs(rows, E);
-  if (st == SFL_E_ARG || !dtype_ok(dtype) || K < 1 || N < 1 || (!offsets && E != 1)) return SFL_E_ARG;
+  if (st == SFL_E_ARG || !result_ok(dtype) || K < 1 || N < 1 || (!offsets && E != 1)) return SFL_E_ARG;
   if (st != SFL_OK || K > kMaxWidth8 || N > kMaxWidth8 || columns > kMaxColumns8) return SFL_E_UNSUPPORTED;
   if (columns % 512 || columns < rows || !dW ||
-      !aligned(dW, dtype == SFL_BF16 ? 2 : 4) || !aligned(Yt, 16) || !aligned(Xt, 16) || !aligned(Ys, 4) ||
+      !aligned(dW, result_size(dtype)) || !aligned(Yt, 16) || !aligned(Xt, 16) || !aligned(Ys, 4) ||
       !aligned(Xs, 4) || (rows > 0 && (!Yt || !Ys || !Xt || !Xs)))
     return SFL_E_ARG;
   const Product8 p{Yt, Ys, Xt, Xs, dW, offsets, rows, N, K, columns, E};
-  return status(launch_product8_weights(p, dtype == SFL_BF16, (hipStream_t)stream));
+  return status(launch_product8_weights(p, dtype, (hipStream_t)stream));
 }
 
 sfl_status_t sfl_adamw_step(const sfl_adamw_t* list, int32_t n, const sfl_adamw_cfg_t* cfg, sfl_stream_t stream) {

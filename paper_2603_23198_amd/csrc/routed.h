@@ -42,8 +42,8 @@ struct Product8 {
   int64_t rows, N, K, columns;
   int E;
 };
-hipError_t launch_product8(const Product8& p, int bf16, hipStream_t s);
-hipError_t launch_product8_weights(const Product8& p, int bf16, hipStream_t s);
+hipError_t launch_product8(const Product8& p, int32_t dtype, hipStream_t s);
+hipError_t launch_product8_weights(const Product8& p, int32_t dtype, hipStream_t s);
 
 hipError_t launch_adamw(const sfl_adamw_t* list, int n, const sfl_adamw_cfg_t& cfg, hipStream_t s);
 

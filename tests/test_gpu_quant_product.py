@@ -336,3 +336,104 @@ def test_tiles_repeat_and_replay():
         g.replay()
         torch.cuda.synchronize()
         assert same_bits(p["Y"].t, want) and (loads != HIGH or same_bits(want, first))
+
+
+def whole(rng, rows, n, first):
+    """Whole numbers that e4m3 holds: of every eight neighbours the first two are 256 and 256 (first) or -256,
+    whose products are far above the others' and cancel; the others are small."""
+    x = rng.integers(-2, 3, size=(rows, n)).astype(np.float64)
+    x[:, 0::8] = 256
+    x[:, 1::8] = 256 if first else -256
+    return x
+
+
+def whole_codes(x, rows_per_scale=1):
+    c = np.zeros((x.shape[0], up(x.shape[1])))
+    c[:, :x.shape[1]] = x
+    return codes_on_gpu(o.to_e4m3(c), np.zeros((-(-x.shape[0] // rows_per_scale), c.shape[1] // 128), int), rows_per_scale)
+
+
+def assert_whole(got, x, w, name=""):
+    """Every partial sum, in any order, is a whole number below 2^24: fp32 sums are exact, and a result is
+    rounded once or not at all."""
+    assert 256 * 256 * x.shape[1] / 4 < 2 ** 23
+    ref = torch.from_numpy(x).cuda() @ torch.from_numpy(w).cuda().t()
+    assert torch.equal(got, ref.to(got.dtype)), f"{name}: {(got != ref.to(got.dtype)).sum().item()} of {got.numel()}"
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("loads,N", [([5], 90), ([70, 0, 33], 200), (LOW, 1901), (HIGH, 1000)])
+def test_sums_lose_nothing_beside_large_products(dt, loads, N):
+    """Few rows, tiles of 128 and of 256 rows."""
+    rng, E = np.random.default_rng(N), len(loads)
+    of, offsets = run_offsets(loads)
+    x, w = whole(rng, sum(loads), 384, True), [whole(rng, N, 384, False) for _ in loads]
+    Q, S, _ = whole_codes(x)
+    W, Ws = zip(*(whole_codes(m, 128)[:2] for m in w))
+    Y = torch.empty((sum(loads), N), dtype=DT[dt], device="cuda")
+    b.sfl_quant_product(Q, S, torch.stack([m.view(torch.uint8) for m in W]).view(Q.dtype), torch.stack(Ws), Y, offsets=offsets)
+    for e in range(E):
+        assert_whole(Y[of[e]:of[e + 1]], x[of[e]:of[e + 1]], w[e], f"expert {e}")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("loads,N,K", [([300, 0, 129], 130, 257), ([40, 0, 200, 129] * 4, 1000, 900)])
+def test_sums_of_weight_gradients_lose_nothing_beside_large_products(dt, loads, N, K):
+    """Tiles of 128 and of 256 rows."""
+    rng = np.random.default_rng(N)
+    of, offsets = run_offsets(loads)
+    columns, at = b.sfl_quant_columns(sum(loads), len(loads)), 0
+    y, x = (np.zeros((n, columns)) for n in (N, K))
+    parts = []
+    for n in loads:
+        parts.append((whole(rng, N, n, True), whole(rng, K, n, False)))
+        y[:, at:at + n], x[:, at:at + n] = parts[-1]
+        at += up(n)
+    (Yt, Ys, _), (Xt, Xs, _) = whole_codes(y), whole_codes(x)
+    dW = torch.empty((len(loads), N, K), dtype=DT[dt], device="cuda")
+    b.sfl_quant_product_weights(Yt, Ys, Xt, Xs, dW, offsets=offsets)
+    for e, (a, c) in enumerate(parts):
+        assert_whole(dW[e], a, c, f"expert {e}")
+
+
+def operands(rng, loads, N, K, kind="normal"):
+    """Rows, and the experts' weights, as the product takes them; their values; offsets."""
+    of, offsets = run_offsets(loads)
+    Q, S, x = codes_on_gpu(*o.quant(operand(rng, sum(loads), K, kind)))
+    W, Ws, w = zip(*(codes_on_gpu(*o.quant_square(operand(rng, N, K, kind)), 128) for _ in loads))
+    W, Ws = torch.stack([m.view(torch.uint8) for m in W]).view(Q.dtype), torch.stack(Ws)
+    return (Q, S, W, Ws), x, w, of, offsets
+
+
+def columns_of(rng, loads, N, K, kind="normal"):
+    """Columns of both sides, NaN behind the last run, and their values."""
+    of, offsets = run_offsets(loads)
+    columns, sides = b.sfl_quant_columns(sum(loads), len(loads)), []
+    for n in (N, K):
+        c, e = o.quant_columns(operand(rng, sum(loads), n, kind), of)
+        codes, exps = np.full((n, columns), 127, np.uint8), np.full((n, columns // 128), 100)
+        codes[:, :c.shape[1]], exps[:, :e.shape[1]] = c, e
+        sides.append(codes_on_gpu(codes, exps)[:2] + (o.held(c, e),))
+    return sides[0], sides[1], offsets
+
+
+@pytest.mark.parametrize("loads,N,K", [([5], 90, 256), (LOW, 1901, 384), (HIGH, 1000, 1152), (HIGH, 513, 128)])
+def test_fast_products(loads, N, K):
+    """Sums from the 8-bit instruction, where asked for: the bound of its 13 bits."""
+    args, x, w, of, offsets = operands(np.random.default_rng(K), loads, N, K, "wide")
+    Y = Out((sum(loads), N), torch.bfloat16)
+    b.sfl_quant_product(*args, Y.t, offsets=offsets, fast=True)
+    got = Y.values()
+    for e in range(len(loads)):
+        assert_product(got[of[e]:of[e + 1]], x[of[e]:of[e + 1]], w[e], "bf16", f"expert {e}")
+
+
+@pytest.mark.parametrize("loads,N,K", [([300, 0, 129], 130, 257), ([40, 0, 200, 129] * 4, 1000, 900)])
+def test_fast_gradients_of_weights(loads, N, K):
+    (Yt, Ys, y), (Xt, Xs, x), offsets = columns_of(np.random.default_rng(N), loads, N, K)
+    dW, at = Out((len(loads), N, K), torch.bfloat16), 0
+    b.sfl_quant_product_weights(Yt, Ys, Xt, Xs, dW.t, offsets=offsets, fast=True)
+    got = dW.values()
+    for e, n in enumerate(loads):
+        assert_product(got[e], y[:, at:at + n], x[:, at:at + n], "bf16", f"expert {e}") if n else np.testing.assert_array_equal(got[e], 0)
+        at += up(n)

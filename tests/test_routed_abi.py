@@ -175,3 +175,27 @@ def test_lists_of_adamw(monkeypatch):
     with pytest.raises(ValueError, match="no scales"):
         b.adamw_list([z(3)], [z(3)], [z(3)], [z(3)], m_scales=[z(1)], v_scales=[z(1)])
     assert len(b.adamw_list([], [], [], [])) == 0
+
+
+def test_fast_products_are_asked_for_and_have_bf16_results():
+    fast = b.SFL_BF16_FAST
+
+    def f(dtype=fast, rows=0, Y=P):
+        return lib.sfl_quant_product(P, P, rows, 128, P, P, 2, 64, P, dtype, Y, None)
+
+    def g(dtype=fast, dW=P, K=64):
+        return lib.sfl_quant_product_weights(P, P, 64, P, P, K, 512, 512, P, 2, dtype, dW, None)
+
+    assert f() == OK and f(Y=P + 2) == OK and f(dtype=0, Y=P + 2) == ARG
+    refused(f, [dict(dtype=0x100), dict(dtype=0x102), dict(Y=P + 1)])
+    refused(g, [dict(dtype=0x100), dict(dtype=0x102), dict(dW=P + 1), dict(dtype=0, dW=P + 2)])
+    assert g(K=(1 << 20) + 1) == UNSUPPORTED
+    # no other call takes it
+    assert lib.sfl_quant_weights(P, fast, 2, 64, 64, P, P, P, P, None) == ARG
+    a = b.QuantArgs(fast, 1, 4, 64, 512, P, None, None, P, P, P, P)
+    assert lib.sfl_quant_rows(a, None) == ARG
+    Q, S, W, Ws = torch.zeros((4, 128)), None, torch.zeros((64, 128)), None
+    with pytest.raises(ValueError, match="bf16 results"):
+        b.sfl_quant_product(Q, S, W, Ws, torch.zeros((4, 64)), fast=True)
+    with pytest.raises(ValueError, match="bf16 results"):
+        b.sfl_quant_product_weights(torch.zeros((64, 512)), None, W, None, torch.zeros((1, 64, 64)), rows=4, fast=True)
