@@ -28,6 +28,13 @@ __device__ __forceinline__ uint32_t order_key(float c) {
 __device__ __forceinline__ float key_value(uint32_t key) {
   return __uint_as_float((key & 0x80000000u) ? (key & 0x7fffffffu) : ~key);
 }
+// The key of a group's worth from those of its one or two best experts (0 for none). Two of the lowest numbers add up
+// to -inf: still above a group without any expert.
+__device__ __forceinline__ uint32_t worth_key(uint32_t b0, uint32_t b1, int group_top) {
+  if (!b0) return 0u;
+  const float w = b1 && group_top == 2 ? key_value(b0) + key_value(b1) : key_value(b0);
+  return max(order_key(w), 1u);
+}
 __device__ __forceinline__ bool available(float l) { return l > -INFINITY; }
 // l - top where both may be +inf
 __device__ __forceinline__ float below(float l, float top) { return l == top ? 0.f : l - top; }
@@ -175,9 +182,7 @@ __global__ __launch_bounds__(kThreads) void k_route_groups_lanes(sfl_route_group
     if (shift > 2) two_most<0x141>(b0, b1);
     if (shift > 3) two_most<0x140>(b0, b1);
     for (int o = 16; o < 1 << shift; o <<= 1) two_most(b0, b1, (uint32_t)__shfl_xor((int)b0, o, 64), (uint32_t)__shfl_xor((int)b1, o, 64));
-    float w = b0 ? key_value(b0) : -INFINITY;
-    if (b1 && a.group_top == 2) w += key_value(b1);
-    const uint32_t worth = x < a.groups << shift ? order_key(w) : 0u;
+    const uint32_t worth = x < a.groups << shift ? worth_key(b0, b1, a.group_top) : 0u;
     // a group is taken where fewer than group_k are worthier, or worth the same before it
     const int group = x >> shift;
     int ahead = 0;
@@ -295,9 +300,7 @@ __global__ __launch_bounds__(kThreads) void k_route_groups_fwd(sfl_route_groups_
         b1 = max(b1, min(b0, k));
         b0 = max(b0, k);
       }
-      float w = b0 ? key_value(b0) : -INFINITY;
-      if (b0 && b1 && a.group_top == 2) w += key_value(b1);
-      worth[wave][g] = b0 ? order_key(w) : 0u;
+      worth[wave][g] = worth_key(b0, b1, a.group_top);
     }
     wave_sync();
     // rounds of the worthiest group; a group that was taken gets the key 0xffffffff

@@ -164,3 +164,32 @@ def test_repeats_and_graphs():
         g.replay()
         torch.cuda.synchronize()
         assert all(same_bits(a, w) for a, w in zip(outs, want))
+
+
+LOWEST = -float(np.finfo(np.float32).max)
+
+
+@pytest.mark.parametrize("E,groups", [(60, 6), (10, 5), (64, 8), (256, 8), (12, 3)])
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+def test_groups_whose_worth_is_below_every_number(E, groups, score):
+    """Biases of the lowest number switch experts off until no others are left. The sum of two of them is -inf:
+    a group of such is the last that is taken, but before a group without any expert, whatever their places."""
+    size = E // groups
+    l = np.random.default_rng(E).normal(size=(5, E))
+    l[1, :size] = -np.inf  # a group without any, before the others and behind them
+    l[2, -size:] = np.nan
+    l[3, size:2 * size] = -np.inf
+    l[4, 1:] = -np.inf
+    kept = np.arange(E) >= E - size // 2 - 1  # some experts of the last group
+    for bias in (np.full(E, LOWEST), np.where(kept, 0.0, LOWEST), np.where(np.arange(E) % size, LOWEST, -3e38)):
+        for group_k in (1, groups - 1, groups):
+            k = min(8, group_k * size)
+            for top in (1, 2):
+                got, want = both(l, "f32", k, bias, score=score, groups=groups, group_k=group_k, group_top=top)
+                check(got, want, k, 1.0)
+
+
+def test_experts_switched_off_by_the_lowest_bias_are_still_there():
+    bias = np.full(60, LOWEST)
+    got, _ = both(np.zeros((1, 60)), "f32", 8, bias, groups=6, group_k=6, group_top=2)
+    assert got[0].tolist() == [list(range(8))]
