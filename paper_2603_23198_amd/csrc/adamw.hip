@@ -192,8 +192,9 @@ __device__ __forceinline__ void turn(const sfl_adamw_t& t, uint64_t place, int64
     if (SMALL) {
       mq[s] = load_codes<ALL>((const uint8_t*)t.m, i, t.n);
       vq[s] = load_codes<ALL>((const uint8_t*)t.v, i, t.n);
-      mb[s] = ALL || i < t.n ? t.m_scale[i / kBlock8] : 127;
-      vb[s] = ALL || i < t.n ? t.v_scale[i / kBlock8] : 127;
+      // 255, which no step writes, would make an infinity: zeros are zeros by any byte
+      mb[s] = min(ALL || i < t.n ? (int)t.m_scale[i / kBlock8] : 127, 254);
+      vb[s] = min(ALL || i < t.n ? (int)t.v_scale[i / kBlock8] : 127, 254);
     } else {
       load_unit4<ALL>((const float*)t.m, i, t.n, m[s]);
       load_unit4<ALL>((const float*)t.v, i, t.n, v[s]);

@@ -293,3 +293,15 @@ def test_moments_in_8_bits_follow_those_in_32():
     ratio = (root8.square().mean() / v32.mean()).sqrt().item()
     # a code is off by a step of at most 1/8; 5120 elements average what the draws add
     assert 0.85 < ratio < 1.15, ratio
+
+
+@pytest.mark.parametrize("byte", [0, 1, 127, 254, 255])
+def test_moments_of_zero_codes_and_any_scale(byte):
+    """Before the first step the codes are zeros, and their scales may be anything."""
+    rng = np.random.default_rng(byte)
+    for n in (5000, 130):
+        x = Tensor(rng, n, small=True, first=True)
+        for s in x.scales:
+            s.bytes.fill_(byte)
+        step([x], 1, seed=2)
+        x.check(1, seed=2)
