@@ -14,6 +14,7 @@
 #include "rows.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 namespace sfl {
@@ -164,9 +165,18 @@ struct Now {  // of this step
   uint32_t key;
 };
 
+// n / d for d from the smallest normal number on, to the nearest fp32 number but where the reals' quotient lies within
+// 2^-45 of itself of the middle of two: the hardware's estimate (one last place off), corrected by what it leaves of
+// n. (8-bit moments, 144 M elements: 474 us, with a division as the compiler writes it 492. The estimate alone costs
+// 468.) The bounds keep a quotient by infinity zero and one that fp32 does not hold infinite.
+__device__ __forceinline__ float quotient(float n, float d) {
+  const float r = __builtin_amdgcn_rcpf(d), q = n * r;
+  const float held = __builtin_amdgcn_fmed3f(q, -FLT_MAX, FLT_MAX);
+  return fmaf(fmaf(-fminf(d, FLT_MAX), held, n), r, q);
+}
+
 // The new moments and parameter of one element, and the root of the second moment, which is rounded to nearest
-// (moments in 8 bits hang on it). The moments round after every operation, as any 32-bit form of the formulas
-// does; the quotient takes the hardware's reciprocal (one last place off; its share of the parameter is lr).
+// (moments in 8 bits hang on it). Every operation rounds to nearest, as in any 32-bit form of the formulas.
 __device__ __forceinline__ float advance(const Hyper& h, const Now& now, const Scale& clip, float decay, float grad,
                                          float& p, float& m, float& v) {
 #pragma clang fp contract(off)
@@ -174,7 +184,7 @@ __device__ __forceinline__ float advance(const Hyper& h, const Now& now, const S
   m = h.beta1 * m + h.rest1 * g;
   v = h.beta2 * v + h.rest2 * (g * g);
   const float root = sqrtf(v);
-  p = p - now.lr * (m * now.inv1 * __builtin_amdgcn_rcpf(root * now.inv2 + h.eps) + decay * p);
+  p = p - now.lr * (quotient(m * now.inv1, root * now.inv2 + h.eps) + decay * p);
   return root;
 }
 

@@ -305,3 +305,24 @@ def test_moments_of_zero_codes_and_any_scale(byte):
             s.bytes.fill_(byte)
         step([x], 1, seed=2)
         x.check(1, seed=2)
+
+
+def test_the_step_is_a_quotient_rounded_once():
+    """beta1 = beta2 = 0, lr = 1 and parameters of zero: m = g and sqrt(v) = |g| without a rounding, so is
+    |g| + eps, and the new parameter is -g / (|g| + eps)."""
+    rng = np.random.default_rng(12)
+    n = 40000
+    g = (rng.integers(1, 1 << 11, size=n) * rng.choice([-1.0, 1.0], size=n)).astype(np.float32)
+    p, m, v = (torch.zeros(n, device="cuda") for _ in range(3))
+    lst = b.adamw_list([p], [torch.from_numpy(g).cuda()], [m], [v])
+    b.sfl_adamw_step(lst, torch.tensor([1], device="cuda"), lr=1.0, beta1=0.0, beta2=0.0, eps=2.0 ** -8)
+    np.testing.assert_array_equal(p.cpu().numpy(), -(g / (np.abs(g) + np.float32(2.0 ** -8))))
+
+
+def test_quotients_beyond_fp32():
+    """m / eps above every fp32 number is an infinite step, one by an infinite root none, inf / inf NaN."""
+    inf = float("inf")
+    m, v = torch.tensor([1e30, -1e30, 1.0, -inf, inf]).cuda(), torch.tensor([0.0, 0.0, inf, 0.0, inf]).cuda()
+    p, g = torch.ones(5, device="cuda"), torch.zeros(5, device="cuda")
+    b.sfl_adamw_step(b.adamw_list([p], [g], [m], [v]), torch.tensor([3], device="cuda"), lr=1e-3, eps=1e-30)
+    np.testing.assert_array_equal(p.cpu().numpy(), [-inf, inf, 1, inf, np.nan])
