@@ -819,7 +819,7 @@ typedef struct {
  * the normal fp32 numbers, lr, weight_decay or max_norm negative or NaN, norm without sumsq. */
 typedef struct {
   double lr, beta1, beta2, eps; /* 1 - beta is formed in 64 bits */
-  double max_norm;              /* not read without sumsq */
+  double max_norm;              /* not read without sumsq; 0 clips all to zero, infinity nothing */
   uint32_t seed;
   uint32_t reserved;
   const int64_t* step;

@@ -695,10 +695,13 @@ def adamw_list(params, grads, m, v, *, halves=None, m_scales=None, v_scales=None
     return a
 
 
-def sfl_adamw_step(tensors, step, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, sumsq=None, max_norm=0.0, norm=None,
+def sfl_adamw_step(tensors, step, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, sumsq=None, max_norm=None, norm=None,
                    lr_scale=None, seed=0, stream=None):
-    cfg = AdamwCfg(lr, beta1, beta2, eps, max_norm, seed & 0xffffffff, 0, _buf(step, _I64, 1), _buf(lr_scale, _F32, 1),
-                   _buf(sumsq, _F64, 1), _buf(norm, _F32, 1))
+    """max_norm: needed with sumsq; math.inf clips nothing (and leaves a step out where the norm is not finite)."""
+    if sumsq is not None and max_norm is None:
+        raise ValueError("sfl_adamw_step: sumsq needs max_norm (math.inf for no clipping)")
+    cfg = AdamwCfg(lr, beta1, beta2, eps, max_norm or 0.0, seed & 0xffffffff, 0, _buf(step, _I64, 1),
+                   _buf(lr_scale, _F32, 1), _buf(sumsq, _F64, 1), _buf(norm, _F32, 1))
     _check("sfl_adamw_step", _lib.sfl_adamw_step(tensors, len(tensors), cfg, _stream(stream)))
 
 

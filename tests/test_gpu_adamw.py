@@ -326,3 +326,13 @@ def test_quotients_beyond_fp32():
     p, g = torch.ones(5, device="cuda"), torch.zeros(5, device="cuda")
     b.sfl_adamw_step(b.adamw_list([p], [g], [m], [v]), torch.tensor([3], device="cuda"), lr=1e-3, eps=1e-30)
     np.testing.assert_array_equal(p.cpu().numpy(), [-inf, inf, 1, inf, np.nan])
+
+
+def test_a_norm_that_clips_nothing():
+    """max_norm = inf: the norm is written and looked at, the gradients are as they are."""
+    rng = np.random.default_rng(13)
+    x = Tensor(rng, 700)
+    out = torch.empty(1, device="cuda")
+    step([x], 3, sumsq=torch.tensor([1e6], dtype=torch.float64, device="cuda"), max_norm=float("inf"), norm=out)
+    assert out.item() == 1e3
+    x.check(3)

@@ -199,3 +199,20 @@ def test_fast_products_are_asked_for_and_have_bf16_results():
         b.sfl_quant_product(Q, S, W, Ws, torch.zeros((4, 64)), fast=True)
     with pytest.raises(ValueError, match="bf16 results"):
         b.sfl_quant_product_weights(torch.zeros((64, 512)), None, W, None, torch.zeros((1, 64, 64)), rows=4, fast=True)
+
+
+def test_a_step_by_the_norm_says_what_it_clips_to(monkeypatch):
+    """Whoever gives the norm, were it to have it written or looked at alone, has to say the largest one: a
+    default of zero would clip every gradient to nothing."""
+    monkeypatch.setattr(b, "_buf", lambda t, *_: None if t is None else P)
+    seen = []
+    monkeypatch.setattr(b, "_lib", type("Lib", (), dict(sfl_adamw_step=lambda _, lst, n, cfg, stream: seen.append(cfg) or 0))())
+    monkeypatch.setattr(b, "_stream", lambda stream: None)
+    step = torch.tensor([1])
+    with pytest.raises(ValueError, match="max_norm"):
+        b.sfl_adamw_step(b.adamw_list([], [], [], []), step, lr=1.0, sumsq=torch.zeros(1))
+    assert not seen
+    b.sfl_adamw_step(b.adamw_list([], [], [], []), step, lr=1.0)
+    for most in (0.0, 1.0, float("inf")):
+        b.sfl_adamw_step(b.adamw_list([], [], [], []), step, lr=1.0, sumsq=torch.zeros(1), max_norm=most)
+        assert seen[-1].max_norm == most
