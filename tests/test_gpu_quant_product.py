@@ -437,3 +437,88 @@ def test_fast_gradients_of_weights(loads, N, K):
     for e, n in enumerate(loads):
         assert_product(got[e], y[:, at:at + n], x[:, at:at + n], "bf16", f"expert {e}") if n else np.testing.assert_array_equal(got[e], 0)
         at += up(n)
+
+
+def assert_exact_products(got, x, w, dt, name=""):
+    """Sums of n exact products in fp32, in any order, and one rounding to dt; on the GPU in float64."""
+    ref = x @ w.t()
+    tol = 2 * U32 * x.shape[1] * (x.abs() @ w.abs().t()) + 1e-37
+    if dt == "bf16":
+        tol += U_BF16 * (ref.abs() + tol)
+    off = (got.double() - ref).abs()
+    assert (off <= tol).all(), f"{name}: worst {(off / tol).nan_to_num(float('inf')).max().item()}"
+
+
+def any_codes(g, *shape, square=False):
+    """Any codes but NaN [..., n] and scales from 2^-6 to 2^6, one for 128 of a row or for 128 x 128, as the products
+    take them; and their values by torch's e4m3."""
+    codes = torch.randint(0, 127, shape, generator=g, device="cuda")
+    codes = (codes + 128 * torch.randint(0, 2, shape, generator=g, device="cuda")).to(torch.uint8).view(torch.float8_e4m3fn)
+    rows, n = shape[-2] if not square else up(shape[-2]) // 128, shape[-1] // 128
+    e = torch.randint(-6, 7, (*shape[:-2], rows, n), generator=g, device="cuda")
+    s = torch.full((*shape[:-2], rows, up(n, 4)), 127, dtype=torch.uint8, device="cuda")
+    s[..., :n] = (e + 127).to(torch.uint8)
+    by = torch.exp2(e.double()).repeat_interleave(128, -1)
+    if square:
+        by = by.repeat_interleave(128, -2)[..., :shape[-2], :]
+    return codes, s, codes.double() * by
+
+
+def run_product(loads, N, K, dt, fast=False):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(N + K)
+    of, offsets = run_offsets(loads)
+    Q, S, x = any_codes(g, sum(loads), K)
+    W, Ws, w = any_codes(g, len(loads), N, K, square=True)
+    Y = Out((sum(loads), N), DT[dt])
+    b.sfl_quant_product(Q, S, W, Ws, Y.t, offsets=offsets, fast=fast)
+    Y.values()
+    for e in range(len(loads)):
+        rows = slice(of[e], of[e + 1])
+        if fast:
+            assert_product(*(t.double().cpu().numpy() for t in (Y.t[rows], x[rows], w[e])), "bf16", f"expert {e}")
+        else:
+            assert_exact_products(Y.t[rows], x[rows], w[e], dt, f"expert {e}")
+
+
+# of 64 experts; the number of columns decides how many parts of k there are
+MANY = [[3, 0, 7, 1, 5, 0, 4, 2] * 8, [10, 0, 25, 1, 3, 31, 8, 2] * 7 + [10, 0, 25, 1, 3, 8, 2, 95]]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("loads", MANY)
+@pytest.mark.parametrize("N", [128, 200, 300, 1034])
+@pytest.mark.parametrize("K", [128, 1152])
+def test_few_rows_in_every_number_of_parts(dt, loads, N, K):
+    """Units of 16 and of 64 rows; 8, 4, 2 and 1 parts of k; one chunk of k and more."""
+    run_product(loads, N, K, dt)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32", "fast"])
+@pytest.mark.parametrize("loads,N", [([130, 5, 0, 257, 31, 400, 128, 129], 6300), ([1100, 0, 513, 900, 700], 5000)])
+@pytest.mark.parametrize("K", [128, 384, 640])
+def test_more_tiles_than_workgroups(dt, loads, N, K):
+    """A workgroup takes tile after tile, the next one's loads under way behind the last one's stores: of 128 and of
+    256 rows, of one step, as many as stages, and more."""
+    run_product(loads, N, K, "bf16" if dt == "fast" else dt, dt == "fast")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32", "fast"])
+@pytest.mark.parametrize("loads,N,K", [([40, 0, 200, 129] * 5, 1000, 1000), ([0, 300, 0, 0, 1, 128, 513], 1600, 1500),
+                                       ([100] * 48, 300, 700)])
+def test_gradients_of_weights_in_many_tiles(dt, loads, N, K):
+    """Tiles of 256 rows, several a workgroup, runs of none and of one block between long ones."""
+    (Yt, Ys, y), (Xt, Xs, x), offsets = columns_of(np.random.default_rng(N), loads, N, K)
+    kind = "f32" if dt == "f32" else "bf16"
+    dW, at = Out((len(loads), N, K), DT[kind]), 0
+    b.sfl_quant_product_weights(Yt, Ys, Xt, Xs, dW.t, offsets=offsets, fast=dt == "fast")
+    dW.values()
+    for e, n in enumerate(loads):
+        if n and dt == "fast":
+            assert_product(dW.t[e].double().cpu().numpy(), y[:, at:at + n], x[:, at:at + n], "bf16", f"expert {e}")
+        elif n:
+            side = [torch.from_numpy(t[:, at:at + n]).cuda() for t in (y, x)]
+            assert_exact_products(dW.t[e], *side, kind, f"expert {e}")
+        else:
+            assert not dW.t[e].any()
+        at += up(n)
