@@ -36,10 +36,9 @@ __device__ __forceinline__ uint32_t codes8(float a, float b, float c, float d) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 
-// A unit of a run: `count` rows from `first` on, all of one expert; `index` units are before it in
-// all, `within` in its run. expert < 0: there is no such unit.
+// A unit of a run: `count` rows from `first` on, all of one expert. expert < 0: there is no such unit.
 struct Unit {
-  int expert, first, count, within;
+  int expert, first, count;
 };
 
 __device__ __forceinline__ int offset8(const int32_t* offsets, int e, int rows) { return min(max(offsets[e], 0), rows); }
@@ -47,13 +46,12 @@ __device__ __forceinline__ int offset8(const int32_t* offsets, int e, int rows) 
 // Unit `index` when every run takes whole units of `size` rows, found by one wave: a lane counts the
 // units of its experts. Offsets are held to [0, rows], a run that descends has no rows.
 __device__ __forceinline__ Unit unit_of(const int32_t* __restrict__ offsets, int E, int rows, int size, int index) {
-  Unit u{-1, 0, 0, 0};
+  Unit u{-1, 0, 0};
   if (!offsets) {
     if ((int64_t)index * size < rows) {
       u.expert = 0;
       u.first = index * size;
       u.count = min(size, rows - u.first);
-      u.within = index;
     }
     return u;
   }
@@ -75,8 +73,7 @@ __device__ __forceinline__ Unit unit_of(const int32_t* __restrict__ offsets, int
     const int n = (max(end - first, 0) + size - 1) / size;
     if (index < before + n) {
       u.expert = e;
-      u.within = index - before;
-      u.first = first + u.within * size;
+      u.first = first + (index - before) * size;
       u.count = min(size, end - u.first);
       return u;
     }
@@ -85,19 +82,6 @@ __device__ __forceinline__ Unit unit_of(const int32_t* __restrict__ offsets, int
     first = end;
     end = offset8(offsets, e + 1, rows);
   }
-}
-
-// Run e in units of `size` rows: its rows and the units before it, by one wave.
-struct Run {
-  int first, count, before;
-};
-__device__ __forceinline__ Run run_of(const int32_t* __restrict__ offsets, int rows, int size, int e) {
-  if (!offsets) return {0, rows, 0};
-  int n = 0;
-  for (int i = lane_id(); i < e; i += kWave)
-    n += (max(offset8(offsets, i + 1, rows) - offset8(offsets, i, rows), 0) + size - 1) / size;
-  const int first = offset8(offsets, e, rows);
-  return {first, max(offset8(offsets, e + 1, rows) - first, 0), wave_sum(n)};
 }
 
 }  // namespace sfl
