@@ -11,6 +11,7 @@
 // root above zero is held as above zero: the denominator of the next step rests on it.
 #include "blocks8.h"
 #include "clip.h"
+#include "order.h"
 #include "rows.h"
 
 #include <algorithm>
@@ -112,18 +113,6 @@ __device__ __forceinline__ void decode(uint32_t w, float by, float (&x)[kUnit]) 
   x[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * by;
 }
 
-template <int CTRL> __device__ __forceinline__ uint32_t dpp_top(uint32_t v) {
-  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false));
-}
-// Largest value over aligned groups of 32 lanes.
-__device__ __forceinline__ uint32_t top32(uint32_t v) {
-  v = dpp_top<0xB1>(v);
-  v = dpp_top<0x4E>(v);
-  v = dpp_top<0x141>(v);
-  v = dpp_top<0x140>(v);
-  return max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
-}
-
 // A scaled magnitude (at most 448) to e4m3's numbers, by 16 bits of noise; exact in e4m3. From 2^-6 on
 // the noise is added below the last of the three mantissa bits, under it (e4m3's subnormal numbers) in
 // steps of 2^-9.
@@ -142,12 +131,12 @@ __device__ __forceinline__ uint32_t encode(const float (&x)[kUnit], const uint32
   float most = 0.f;  // a NaN has no part in it
 #pragma unroll
   for (int j = 0; j < kUnit; ++j) most = fmaxf(most, fabsf(x[j]));
-  uint32_t top = top32(__float_as_uint(most));
+  uint32_t top = group_max<32>(__float_as_uint(most));
   if (top == 0x7f800000u) {  // an infinity: once more without those
     top = 0;
 #pragma unroll
     for (int j = 0; j < kUnit; ++j) top = max(top, magnitude8(x[j]));
-    top = top32(top);
+    top = group_max<32>(top);
   }
   *byte = scale_byte8(top);
   const float by = inverse8(*byte);

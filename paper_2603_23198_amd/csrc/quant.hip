@@ -6,6 +6,7 @@
 // unpacked 190, two waves and 70 us); 4096 x 16384 fp32 in squares, both
 // layouts, 80 us (5.1).
 #include "blocks8.h"
+#include "order.h"
 #include "rows.h"
 
 #include <algorithm>
@@ -15,17 +16,6 @@ namespace sfl {
 namespace {
 
 constexpr int kThreads = 256;
-
-template <int CTRL> __device__ __forceinline__ uint32_t dpp_top(uint32_t v) {
-  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false));
-}
-// Largest value over aligned groups of 16 lanes, in every lane.
-__device__ __forceinline__ uint32_t top16(uint32_t v) {
-  v = dpp_top<0xB1>(v);
-  v = dpp_top<0x4E>(v);
-  v = dpp_top<0x141>(v);
-  return dpp_top<0x140>(v);
-}
 
 // Largest magnitude so far and of eight elements; a NaN has no part in it (fmaxf leaves it out), an infinity
 // has: where one shows, the caller counts again without those (see finite_top).
@@ -41,8 +31,8 @@ __device__ __forceinline__ uint32_t finite_most(uint32_t top, const float (&x)[8
 }
 // The bits of the largest finite magnitude of 16 lanes' eight elements each.
 __device__ __forceinline__ uint32_t top_of_row(const float (&x)[8]) {
-  uint32_t top = top16(__float_as_uint(most(0.f, x)));
-  if (top == 0x7f800000u) top = top16(finite_most(0u, x));
+  uint32_t top = group_max<16>(__float_as_uint(most(0.f, x)));
+  if (top == 0x7f800000u) top = group_max<16>(finite_most(0u, x));
   return top;
 }
 
@@ -268,7 +258,7 @@ __global__ __launch_bounds__(kThreads) void k_quant_tile(TileArgs a) {
     if (SQUARE) {
 #pragma unroll
       for (int j = 1; j < 8; ++j) col[0] = max(col[0], col[j]);
-      col[0] = top16(col[0]);
+      col[0] = group_max<16>(col[0]);
     }
     // over the wave's 32 rows, then over all
     if (SQUARE || a.Qt) {

@@ -14,6 +14,7 @@
 // kernel alone: 45 us with 64-bit keys traded over LDS, 9.4 us with a lane per expert and the wave's
 // largest key in a scalar register.
 #include "block.h"
+#include "order.h"
 #include "rows.h"
 
 #include <algorithm>
@@ -23,34 +24,6 @@ namespace sfl {
 namespace {
 
 constexpr int kThreads = 256;
-
-// A logit's place in the order of the reals as an unsigned number: larger logit, larger key; 0
-// for an unavailable one (-inf or NaN). -0 and +0 have one key.
-__device__ __forceinline__ uint32_t order_key(float l) {
-  if (!(l > -INFINITY)) return 0u;
-  const uint32_t u = __float_as_uint(l + 0.f);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-__device__ __forceinline__ float key_logit(uint32_t key) {
-  return __uint_as_float((key & 0x80000000u) ? (key & 0x7fffffffu) : ~key);
-}
-
-template <int CTRL> __device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
-  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false));
-}
-
-// Largest value of aligned groups of G lanes, in every lane (lanes trade as in group_sum).
-template <int G> __device__ __forceinline__ uint32_t group_max(uint32_t v) {
-  if (G >= 2) v = dpp_max<0xB1>(v);
-  if (G >= 4) v = dpp_max<0x4E>(v);
-  if (G >= 8) v = dpp_max<0x141>(v);
-  if (G >= 16) v = dpp_max<0x140>(v);
-  if (G == 32) v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
-  if (G == 64)
-    v = max(max((uint32_t)readlane_i((int)v, 0), (uint32_t)readlane_i((int)v, 16)),
-            max((uint32_t)readlane_i((int)v, 32), (uint32_t)readlane_i((int)v, 48)));
-  return v;
-}
 
 // A lane's experts e0 .. e0 + PL - 1 of a row of E, by one load where all are there; what is past
 // the end is not available.
@@ -108,7 +81,7 @@ __global__ __launch_bounds__(kThreads) void k_route_fwd(const V* __restrict__ lo
       }
     }
   }
-  const float top = key_logit(top_key);
+  const float top = key_value(top_key);
   float ex[PL], Z = 0.f;
 #pragma unroll
   for (int i = 0; i < PL; ++i) {
@@ -168,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(const V* __restrict__ lo
     counts[i] = key != 0u && (chosen[i] || !normalise);
     top_key = max(top_key, counts[i] ? key : 0u);
   }
-  const float top = key_logit(group_max<G>(top_key));
+  const float top = key_value(group_max<G>(top_key));
   float p[PL], Z = 0.f, mean = 0.f;
 #pragma unroll
   for (int i = 0; i < PL; ++i) {

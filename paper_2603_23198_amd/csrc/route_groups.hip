@@ -10,6 +10,7 @@
 //   sigmoid:             w_j = scale s_j,         dl_j = s_j G_j sigmoid(-l_j),     G = scale dw
 //   softmax, normalised: as a softmax over the chosen; else p over all: dl_i = p_i (up_i - sum p up)
 #include "blocks8.h"
+#include "order.h"
 #include "rows.h"
 
 #include <algorithm>
@@ -20,14 +21,6 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 
-__device__ __forceinline__ uint32_t order_key(float c) {
-  if (!(c > -INFINITY)) return 0u;
-  const uint32_t u = __float_as_uint(c + 0.f);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-__device__ __forceinline__ float key_value(uint32_t key) {
-  return __uint_as_float((key & 0x80000000u) ? (key & 0x7fffffffu) : ~key);
-}
 // The key of a group's worth from those of its one or two best experts (0 for none). Two of the lowest numbers add up
 // to -inf: still above a group without any expert.
 __device__ __forceinline__ uint32_t worth_key(uint32_t b0, uint32_t b1, int group_top) {
@@ -51,10 +44,6 @@ __device__ __forceinline__ float wave_topf(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
   return v;
-}
-
-template <int CTRL> __device__ __forceinline__ uint32_t dpp_most(uint32_t v) {
-  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false));
 }
 
 // The two largest of two lanes' two largest each.
@@ -95,17 +84,6 @@ __device__ __forceinline__ double inverse64(double d) {
   return fma(y, fma(-d, y, 1.0), y);
 }
 
-template <int G> __device__ __forceinline__ uint32_t group_top(uint32_t v) {  // largest over aligned groups of lanes
-  if (G >= 2) v = dpp_most<0xB1>(v);
-  if (G >= 4) v = dpp_most<0x4E>(v);
-  if (G >= 8) v = dpp_most<0x141>(v);
-  if (G >= 16) v = dpp_most<0x140>(v);
-  if (G == 32) v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
-  if (G == 64)
-    v = max(max((uint32_t)readlane_i((int)v, 0), (uint32_t)readlane_i((int)v, 16)),
-            max((uint32_t)readlane_i((int)v, 32), (uint32_t)readlane_i((int)v, 48)));
-  return v;
-}
 template <int G> __device__ __forceinline__ double group_sum64(double v) {
 #pragma unroll
   for (int o = 1; o < G; o <<= 1) v += __shfl_xor(v, o, 64);
@@ -148,7 +126,7 @@ __global__ __launch_bounds__(kThreads) void k_route_groups_lanes(sfl_route_group
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < PL; ++i) m = max(m, order_key(l[i]));
-    m = group_top<G>(m);
+    m = group_max<G>(m);
     top = m ? key_value(m) : -INFINITY;
   }
   double s[PL];
@@ -203,7 +181,7 @@ __global__ __launch_bounds__(kThreads) void k_route_groups_lanes(sfl_route_group
   }
   int found = 0;
   for (int j = 0; j < a.k; ++j) {
-    const uint32_t m = group_top<G>(best);
+    const uint32_t m = group_max<G>(best);
     const uint64_t have = ballot(best == m);
     found += m != 0u;
     if (m && best == m && !(have & before)) {
@@ -232,7 +210,7 @@ __global__ __launch_bounds__(kThreads) void k_route_groups_lanes(sfl_route_group
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < PL; ++i) m = max(m, round[i] >= 0 ? order_key(l[i]) : 0u);
-    m = group_top<G>(m);
+    m = group_max<G>(m);
     const float high = m ? key_value(m) : -INFINITY, held = fminf(high, 0.f), shifted = softmax ? 0.f : expf(held);
     sum = 0.f;
 #pragma unroll
