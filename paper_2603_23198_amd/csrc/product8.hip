@@ -547,30 +547,47 @@ int64_t most_units(const Product8& p, int64_t size) {
 
 }  // namespace
 
-// Which kernel, at K = 4096 in bf16 (kernel traces, µs; K weighs on all alike):
-//   rows x columns, experts      few rows   tiles of 128   tiles of 256
-//   64 x 4096, 1                    15.6        28.0
-//   128 x 4096, 1                   20.2        29.1
-//   256 x 4096, 1                   36.4        29.1
-//   64 x 8192, 2                    25.6        28.6
-//   128 x 8192, 2                   29.4        28.6
-//   128 x 4096, 8 (16 rows each)    29.6        30.8           47.1
-//   256 x 4096, 8                   35.5        33.0           48.6
-//   2048 x 4096, 8                              46.2           59.4
-//   4096 x 4096, 8                              78.3           64.2
-// The kernel for few rows costs what it has of results, the tiles what one round of them does; where runs are
-// short it reads every weight once, which no tile does cheaper.
+// Which kernel, at K = 4096 in bf16 (µs a call, captured, over several sets of buffers; K weighs on all alike):
+//                                                      exact products        8-bit instruction
+//   rows x columns, experts      few rows   tiles of 128        of 256         128       256
+//   64 x 4096, 1                   15           54           89             29        44
+//   256 x 4096, 1                  29           54           92             30        47
+//   512 x 4096, 1                  39           56           92             30        47
+//   256 x 8192, 2                  43           56           92             34        47
+//   64 x 4096, 8                   34           55           91             37        50
+//   512 x 4096, 8                  47           55           92             41        52
+//   1024 x 4096, 8                 81           58           95             45        55
+//   2048 x 4096, 8                              66          100             49        65
+//   4096 x 4096, 8                             126          118             87        68
+//   16384 x 4096, 8                            480          426            305       252
+//   12288 x 64, 1                  35           55           93
+// The kernel for few rows costs what it has of results, the tiles what one round of them does, twice as much with
+// exact products; where runs are short it reads every weight once, which no tile does cheaper.
+bool few_rows(const Product8& p, int32_t dtype, int64_t live) {
+  return p.rows <= 16 * live || p.rows * p.N <= (dtype == SFL_BF16_FAST ? 3 << 18 : 1 << 21);
+}
+// Tiles of 256 rows read a third less, but a round of them (one a CU) takes as long as 1.6 rounds of 128. Runs end
+// half a tile short on average.
+bool high_tiles(const Product8& p, int64_t live) {
+  auto rounds = [&](int64_t size) {
+    const double units = p.offsets ? (double)p.rows / size + live / 2.0 : (double)cdiv(p.rows, size);
+    return std::max(1.0, units * cdiv(p.N, kTileN) / device_cus());
+  };
+  return rounds(256) < 0.62 * rounds(128);
+}
+
 hipError_t launch_product8(const Product8& p, int32_t dtype, hipStream_t s) {
   const bool bf16 = dtype != SFL_F32;
   const int64_t live = std::min<int64_t>(p.E, p.rows);
-  if (p.rows <= 16 * live || p.rows * p.N <= 3 << 18) {
-    // two workgroups a CU at least; parts of k beyond that only add sums (64 rows of eight experts: 37, 31 and 41 us
-    // in one, two and four parts)
-    const int64_t waves = live * cdiv(p.N, 16), want = (int64_t)device_cus() * 16;
-    const int ks = waves * 8 <= want ? 8 : waves * 4 <= want ? 4 : waves * 2 <= want ? 2 : 1;
+  if (few_rows(p, dtype, live)) {
     // 16 rows a unit take fewer registers and less LDS; runs of more rows would read their weights once more
-    // for every 16 (8 to 128 rows of eight experts: 30 us either way)
-    if (p.rows <= 4 * live) {
+    // for every 16 (8 to 128 rows of eight experts: 35 us either way)
+    const bool short_runs = p.rows <= 4 * live;
+    // two workgroups a CU at least; parts of k beyond that only add sums (64 rows of eight experts: 37, 31 and 41 us
+    // in one, two and four parts; 12288 rows of 64 columns: 39, 30, 34 and 47 in one to eight)
+    const int64_t waves = std::max(live, cdiv(p.rows, short_runs ? 16 : 64)) * cdiv(p.N, 16), want = (int64_t)device_cus() * 16;
+    const int ks = waves * 8 <= want ? 8 : waves * 4 <= want ? 4 : waves * 2 <= want ? 2 : 1;
+    if (short_runs) {
       const int64_t units = most_units(p, 16);
       return ks == 8 ? stream<1, 8>(p, bf16, units, s) : ks == 4 ? stream<1, 4>(p, bf16, units, s)
            : ks == 2 ? stream<1, 2>(p, bf16, units, s) : stream<1, 1>(p, bf16, units, s);
@@ -579,7 +596,7 @@ hipError_t launch_product8(const Product8& p, int32_t dtype, hipStream_t s) {
     return ks == 8 ? stream<4, 8>(p, bf16, units, s) : ks == 4 ? stream<4, 4>(p, bf16, units, s)
          : ks == 2 ? stream<4, 2>(p, bf16, units, s) : stream<4, 1>(p, bf16, units, s);
   }
-  const bool high = p.rows / p.E >= 512;
+  const bool high = high_tiles(p, live);
   const int64_t count = most_units(p, high ? 256 : 128) * cdiv(p.N, kTileN);
   return high ? tiles_of<256, false>(p, dtype, count, s) : tiles_of<128, false>(p, dtype, count, s);
 }

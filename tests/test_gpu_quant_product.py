@@ -260,8 +260,8 @@ def test_a_row_does_not_depend_on_its_place():
     assert same_bits(out[0][turn], out[1])
 
 
-# Results of more than 768 K values in runs of more than 16 rows come from tiles: of 128 rows, from 512 rows a
-# run on of 256.
+# Fast results of more than 768 K values in runs of more than 16 rows come from tiles, others of more than 2 M
+# (below: TILES).
 LOW, HIGH = [130, 5, 0, 257, 31], [700, 513, 1, 900]
 
 
@@ -522,3 +522,87 @@ def test_gradients_of_weights_in_many_tiles(dt, loads, N, K):
         else:
             assert not dW.t[e].any()
         at += up(n)
+
+
+# Runs and columns whose results come from tiles, in few and in several rounds of the compute units: of 128 and of
+# 256 rows.
+TILES = [([130, 5, 0, 257, 31], 5003), ([700, 513, 1, 900], 8300)]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32", "fast"])
+@pytest.mark.parametrize("loads,N", TILES)
+@pytest.mark.parametrize("K", [128, 256, 512, 1152])
+def test_tiles_of_both_heights(dt, loads, N, K):
+    """One to nine steps, rows and columns that end inside a tile."""
+    run_product(loads, N, K, "bf16" if dt == "fast" else dt, dt == "fast")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32", "fast"])
+@pytest.mark.parametrize("loads,N", TILES)
+def test_tiles_of_both_heights_with_rows_of_no_expert_and_numbers_that_are_not_finite(dt, loads, N):
+    """Runs that begin behind the first row and end before the last; a NaN reaches its row or column and no other."""
+    g, rows = torch.Generator(device="cuda"), sum(loads) + 70
+    g.manual_seed(N)
+    of, offsets = run_offsets(loads, 9)
+    Q, S, x = any_codes(g, rows, 384)
+    W, Ws, w = any_codes(g, len(loads), N, 384, square=True)
+    for codes, values, at in ((Q, x, (of[1] - 1, 77)), (W, w, (len(loads) - 1, N - 1, 200))):
+        codes.view(torch.uint8)[at] = 127
+        values[at] = float("nan")
+    Y = Out((rows, N), torch.float32 if dt == "f32" else torch.bfloat16)
+    b.sfl_quant_product(Q, S, W, Ws, Y.t, offsets=offsets, fast=dt == "fast")
+    Y.values()
+    assert (Y.t[:9] == -77).all() and (Y.t[of[-1]:] == -77).all()
+    for e in range(len(loads)):
+        if not loads[e]:
+            continue
+        got, ref, size = Y.t[of[e]:of[e + 1]].double(), x[of[e]:of[e + 1]] @ w[e].t(), x[of[e]:of[e + 1]].abs() @ w[e].abs().t()
+        want = torch.zeros_like(got, dtype=torch.bool)
+        if e == 0:
+            want[-1] = True
+        if e == len(loads) - 1:
+            want[:, -1] = True
+        assert torch.equal(got.isnan(), want)
+        # of all products' magnitudes: fp32 sums, or 13 bits of each eight; and the result's rounding
+        tol = size * (2 * U32 * 384 + (8 * 2.0 ** -13 if dt == "fast" else 0)) + (0 if dt == "f32" else U_BF16 * 1.01) * ref.abs() + 1e-37
+        assert ((got - ref).abs() <= tol)[~want].all()
+
+
+@pytest.mark.parametrize("fast", [False, True])
+@pytest.mark.parametrize("loads,N", TILES)
+def test_tiles_of_both_heights_repeat_and_replay(loads, N, fast):
+    """Captured, on batches of other loads, offsets without meaning among them: the bits of the eager calls."""
+    g, rows, E = torch.Generator(device="cuda"), sum(loads), len(loads)
+    g.manual_seed(N)
+    of, offsets = run_offsets(loads)
+    Q, S, _ = any_codes(g, rows, 384)
+    W, Ws, _ = any_codes(g, E, N, 384, square=True)
+    Y = Out((rows, N), torch.bfloat16)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.sfl_quant_product(Q, S, W, Ws, Y.t, offsets=offsets, fast=fast)
+    others = [loads, [0] * (E - 1) + [rows], [1] * (E - 1) + [rows - E + 1], [rows // E] * E]
+    for new in [run_offsets(n)[0] for n in others] + [[rows // 2, 20, 90, 10, rows, 5][:E + 1], [-5, 3 * rows, 7, rows, 1 << 30, 0][:E + 1]]:
+        offsets.copy_(torch.tensor(new))
+        seen = []
+        for call in (lambda: b.sfl_quant_product(Q, S, W, Ws, Y.t, offsets=offsets, fast=fast), graph.replay):
+            Y.t.fill_(-77)
+            call()
+            torch.cuda.synchronize()
+            Y.values()
+            seen.append(Y.t.clone())
+        # runs that overlap write some rows twice, in any order
+        assert same_bits(*seen) or sorted(new) != new
+
+
+@pytest.mark.parametrize("rows,N", [(1100, 2000), (4200, 4200)])
+def test_tiles_of_both_heights_without_offsets(rows, N):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(N)
+    Q, S, x = any_codes(g, rows, 640)
+    W, Ws, w = any_codes(g, N, 640, square=True)
+    for dt in ("bf16", "f32"):
+        Y = Out((rows, N), DT[dt])
+        b.sfl_quant_product(Q, S, W, Ws, Y.t)
+        Y.values()
+        assert_exact_products(Y.t, x, w, dt)
