@@ -644,7 +644,7 @@ enum {
  *   chosen where it is available and c_e is neither -inf nor NaN
  *   The experts are `groups` runs of E / groups. With more than one, a group's worth is the sum (in
  *   fp32) of its group_top largest c (of fewer where it has fewer; a group without any is not
- *   taken), and the experts of the group_k worthiest groups can be chosen.
+ *   taken, and below one whose sum is -inf), and the experts of the group_k worthiest groups can be chosen.
  *   expert [T][k] int32: those with the k largest c, in that order; -1 where fewer can be chosen
  *   weight [T][k] fp32: scale s_j / (sum of s over the chosen experts) with normalise = 1, else
  *          scale s_j; 0 where expert is -1. Where the scores underflow, their quotients are still those
@@ -743,7 +743,7 @@ sfl_status_t sfl_quant_weights(const void* W, sfl_dtype_t dtype, int64_t E, int6
  *   Y[t][n] = sum_k x[t][k] w[e][n][k]
  * summed in fp32 on the matrix cores, from exact products, and rounded once to dtype. Exact are scales from 2^-117
  * on and numbers below 2^127. With BF16_FAST the results are bf16, and where there are many rows the products
- * come from the 8-bit matrix instruction, at up to twice the rate: it adds those of eight neighbouring k with 13
+ * come from the 8-bit matrix instruction, at up to 1.8 times the rate: it adds those of eight neighbouring k with 13
  * bits below the largest of them and drops the rest (1.6e-5 of the result for normal operands; small products
  * beside large ones that cancel are lost).
  *  Q, S     x: rows as sfl_quant_rows has them, [rows][K] and their scales, K a multiple of 128
@@ -814,9 +814,10 @@ typedef struct {
  * the list (every tensor counted as whole blocks of 128), the lower 16 bits are added below the last bit that
  * m keeps and the upper 16 below that of sqrt(v), and what is below is cut off. A root above zero never becomes
  * zero. Moments that are not finite are held as NaN, and no others.
- * Errors: SFL_E_ARG for n < 0, a NULL list (n > 0), cfg or step, a NULL buffer of a tensor with elements, scales
- * missing or given for fp32 moments, an unknown type, a half of bf16 parameters, betas outside [0, 1), eps below
- * the normal fp32 numbers, lr, weight_decay or max_norm negative or NaN, norm without sumsq. */
+ * Errors: SFL_E_ARG for n < 0, a tensor of more than 2^40 elements, a NULL list (n > 0), cfg or step, a NULL buffer
+ * of a tensor with elements, scales missing or given for fp32 moments, an unknown type, a half of bf16 parameters,
+ * betas outside [0, 1), eps below the normal fp32 numbers, lr, weight_decay or max_norm negative or NaN, norm
+ * without sumsq. */
 typedef struct {
   double lr, beta1, beta2, eps; /* 1 - beta is formed in 64 bits */
   double max_norm;              /* not read without sumsq; 0 clips all to zero, infinity nothing */

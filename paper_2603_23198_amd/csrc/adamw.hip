@@ -1,8 +1,8 @@
 // One step of AdamW over a list of tensors: every element of parameter, gradient and moments is read
 // once and written once, and the clipping coefficient comes from the gradients' squared norm on the
 // device, so that clipping costs no pass of its own. Bound by memory: 30 bytes an element with fp32
-// gradients and moments and the bf16 copy (2^27 elements 729 us, 5.5 TB/s), 16 with bf16 gradients and moments in 8
-// bits (144 M elements 472 us, 4.9 TB/s; some 90 instructions an element are not far behind).
+// gradients and moments and the bf16 copy (2^27 elements 735 to 755 us, 5.3 to 5.5 TB/s), 16 with bf16 gradients and
+// moments in 8 bits (144 M elements 474 to 487 us, 4.7 to 4.85 TB/s; some 95 instructions an element are not far behind).
 //
 // Moments in 8 bits: e4m3 codes with a power of two for each 128 elements (of v the root, which has
 // half the range). Three mantissa bits are coarser than what a slow average moves in a step (v by 1 part

@@ -2,9 +2,10 @@
 //   C[m][n] = sum_b 2^(sa[m][b] + sb[n][b]) sum_{k in block b} A[m][k] B[n][k]
 // Rows of the result are the rows of an expert's run, or (the weights' gradients) the sum runs over the
 // run's tokens. Codes become bf16 with their scale by one instruction for two of them, exactly for scales from
-// 2^-117 on, and bf16 products are exact in the fp32 sums of the matrix cores. (The 8-bit matrix
-// instructions are not: they add the products of eight neighbouring k with 13 bits below the largest of
-// them, 1.6e-5 of the result's magnitude for normal operands, by measurement. A caller may ask for them.)
+// 2^-117 on, and bf16 products are exact in the fp32 sums of the matrix cores. The 8-bit matrix instructions
+// are not: they add the products of eight neighbouring k with 13 bits below the largest of them, by measurement
+// (1.6e-5 of the result's magnitude for normal operands). They are up to 1.8 times as fast and serve bf16 results of
+// many rows, and gradients, of a caller who asks for that (BF16_FAST).
 #include "blocks8.h"
 #include "direct.h"
 #include "rows.h"
@@ -40,8 +41,9 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 // Chunk c (16 k) of row r lies at position c ^ swizzle(r), so that the 8 lanes of a fragment read's phase
 // meet 8 different positions. Scales travel the same way, a word of four blocks per row.
 // A workgroup stays on its CU and takes tile after tile; the next tile's first stage is on its way while
-// the results of one are stored. 16384 x 4096 x 4096 over eight experts: 283 us, 1.94 PFLOP/s on the 8-bit instruction
-// (a library product of 8192^3 reaches 2.66); the fp32 gradients of their weights, in bf16, 495 us, 1.11 PFLOP/s.
+// the results of one are stored. 16384 x 4096 x 4096 over eight experts of uneven load, exact products: 491 us in bf16, 507
+// in fp32 (1.11 PFLOP/s; a library product in bf16 of 8192^3 reaches 1.24 to 1.48), the gradients of their weights 464 and 495.
+// On the 8-bit instruction 276 and 294 (1.99 PFLOP/s; the library's 2.66). Loads in whole tiles: 426 and 252.
 constexpr int kTileN = 256, kTileThreads = 512, kTileWaves = 8, kStep = 128;
 constexpr int kWordRing = 4;  // scale words: the one in use, and up to two ahead of it
 
@@ -566,8 +568,8 @@ int64_t most_units(const Product8& p, int64_t size) {
 bool few_rows(const Product8& p, int32_t dtype, int64_t live) {
   return p.rows <= 16 * live || p.rows * p.N <= (dtype == SFL_BF16_FAST ? 3 << 18 : 1 << 21);
 }
-// Tiles of 256 rows read a third less, but a round of them (one a CU) takes as long as 1.6 rounds of 128. Runs end
-// half a tile short on average.
+// Tiles of 256 rows read a third less, but a round of them (one a CU) takes as long as 1.6 rounds of 128. Runs end half
+// a tile short on average.
 bool high_tiles(const Product8& p, int64_t live) {
   auto rounds = [&](int64_t size) {
     const double units = p.offsets ? (double)p.rows / size + live / 2.0 : (double)cdiv(p.rows, size);
@@ -601,7 +603,8 @@ hipError_t launch_product8(const Product8& p, int32_t dtype, hipStream_t s) {
   return high ? tiles_of<256, false>(p, dtype, count, s) : tiles_of<128, false>(p, dtype, count, s);
 }
 
-// The higher tiles where they fill the CUs: they read a quarter less.
+// The higher tiles where they fill the CUs: they read a third less (4096 rows, 4096 x 4096, eight experts: 206 us in fp32 against
+// 257; 2048 rows, 768 x 1024, where 96 of them leave most CUs idle: 32 against 14).
 hipError_t launch_product8_weights(const Product8& p, int32_t dtype, hipStream_t s) {
   const int64_t high = p.E * cdiv(p.N, 256) * cdiv(p.K, kTileN), low = p.E * cdiv(p.N, 128) * cdiv(p.K, kTileN);
   return high >= device_cus() ? tiles_of<256, true>(p, dtype, high, s) : tiles_of<128, true>(p, dtype, low, s);

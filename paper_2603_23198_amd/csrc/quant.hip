@@ -3,7 +3,7 @@
 // along a row (k_quant_rows), along a row and along a run's tokens at once, or in squares of 128 x 128
 // (k_quant_tile). Bound by memory: every element is read once for both layouts. 16384 x 4096 bf16: rows
 // 40 us (5.0 TB/s), both layouts 64 (4.2; 158 registers, three waves a SIMD; with a tile's elements kept
-// unpacked 190, two waves and 70 us); 4096 x 16384 fp32 in squares, both
+// unpacked 190, two waves and 70 us), of fp32 rows 88 (4.6); 4096 x 16384 fp32 in squares, both
 // layouts, 80 us (5.1).
 #include "blocks8.h"
 #include "order.h"
